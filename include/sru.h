@@ -331,6 +331,87 @@ SRU_API int sru_scan_backward(const float* U, const float* X, const float* C, co
                       void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Operators of a language model around the layer.  The conventions above
+ * hold, except that activations and logits are fp32 or bf16 (sru_dtype; bf16
+ * values as raw bits, rounded to nearest even once, on output) and may be
+ * strided as each call says.  Parameters, states, row statistics and losses
+ * are fp32, and so is all arithmetic.
+ * ------------------------------------------------------------------------- */
+typedef enum { SRU_DTYPE_FP32 = 0, SRU_DTYPE_BF16 = 1 } sru_dtype;
+
+/* Vocabulary rows: logits [N, V], row pitch ld >= V elements, columns
+ * contiguous, at a temperature T > 0 (finite):
+ *   m = max_j z_j,  S = sum_j exp((z_j - m) / T),
+ *   log p_j = (z_j - m) / T - log S
+ * stats [N, 2] holds (m, S) for the gradient calls.  Logits may be -inf (a
+ * token that is not possible: p = 0, no gradient) or the type's lowest value.
+ * A row whose logits are all -inf has log p = -inf everywhere, entropy 0 and
+ * a gradient of zeros.  A row with a NaN or +inf has NaN results.
+ *
+ * sru_token_logprobs:
+ *   tokens [N] int64: the given token of each row; one outside 0 .. V-1 marks
+ *     a row that is not scored (log probability 0, no gradient from it)
+ *   logprob [N];  entropy [N] = -sum_j p_j log p_j
+ *   top_ids [N, top] int64, top_logprobs [N, top]: the `top` largest logits
+ *     (0 <= top <= SRU_MAX_TOP and <= V; NULL with top = 0), best first,
+ *     equal ones by the lower token; a NaN is no alternative, and where a row
+ *     has fewer numbers than `top` the rest are (-1, -inf)
+ * sru_token_logprobs_backward: the gradient with respect to the logits of
+ *     sum_n dlogprob_n logprob_n + dentropy_n entropy_n
+ *           + sum_k dtop_nk top_logprobs_nk
+ *   given the forward call's stats, entropy and top_ids.  dlogprob, dentropy
+ *   and dtop may each be NULL (no gradient; entropy, top_ids are then not
+ *   read).  dlogits [N, V], row pitch ldd >= V, the logits' type; it may be
+ *   the logits' own memory (the same pointer and pitch). */
+#define SRU_MAX_TOP 64
+SRU_API size_t sru_token_logprobs_workspace_bytes(int N, int V, int dtype, int top);
+SRU_API int sru_token_logprobs(const void* logits, long long ld, int dtype,
+                               const int64_t* tokens, int N, int V, int top, float temperature,
+                               float* logprob, float* entropy, float* stats, int64_t* top_ids,
+                               float* top_logprobs, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
+SRU_API int sru_token_logprobs_backward(const void* logits, long long ld, int dtype,
+                                        const int64_t* tokens, const float* stats,
+                                        const float* entropy, const float* dlogprob,
+                                        const float* dentropy, const int64_t* top_ids,
+                                        const float* dtop, int N, int V, int top,
+                                        float temperature, void* dlogits, long long ldd,
+                                        hipStream_t stream);
+
+/* Distillation from a teacher's top logits: q = softmax(z / T) of the student's
+ * row, p = softmax(t / T) over the row's kept teacher entries,
+ *   loss_n = sum_k p_k (log p_k - log q_{id_k})
+ *   teacher_ids [N, K] int64, teacher_logits [N, K] (teacher_dtype), both
+ *     contiguous, 1 <= K <= SRU_MAX_TEACHER.  An entry whose id is outside
+ *     0 .. V-1, or whose logit is -inf, is not kept; a row with none has loss
+ *     0 and a gradient of zeros.  An id that occurs twice counts as both.
+ *   loss [N]: +inf where the student gives a kept entry no probability
+ * The gradient with respect to the logits, given the weight dloss [N] of each
+ * row's loss, is dloss_n / T (q_j sum_k p_k - sum_{k: id_k = j} p_k).
+ * sru_distill_backward takes it from the forward call's stats;
+ * sru_distill_forward_backward does both (for callers that know the weights
+ * beforehand, e.g. 1 / rows) and reads the logits from memory once where a
+ * row fits the caches.  dlogits as above; it may be the logits' own memory. */
+#define SRU_MAX_TEACHER 1024
+SRU_API size_t sru_distill_workspace_bytes(int N, int V, int dtype);
+SRU_API int sru_distill_forward(const void* logits, long long ld, int dtype,
+                                const int64_t* teacher_ids, const void* teacher_logits,
+                                int teacher_dtype, int N, int V, int K, float temperature,
+                                float* loss, float* stats, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream);
+SRU_API int sru_distill_backward(const void* logits, long long ld, int dtype,
+                                 const int64_t* teacher_ids, const void* teacher_logits,
+                                 int teacher_dtype, const float* stats, const float* dloss, int N,
+                                 int V, int K, float temperature, void* dlogits, long long ldd,
+                                 hipStream_t stream);
+SRU_API int sru_distill_forward_backward(const void* logits, long long ld, int dtype,
+                                         const int64_t* teacher_ids, const void* teacher_logits,
+                                         int teacher_dtype, const float* dloss, int N, int V,
+                                         int K, float temperature, float* loss, float* stats,
+                                         void* dlogits, long long ldd, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Measurement hook, per calling thread.  sru_timing_begin arms it with
  * `capacity` events the caller created (hipEventCreate, timing enabled).
  * Every kernel this thread then enqueues through the calls above is
@@ -346,7 +427,10 @@ SRU_API int sru_scan_backward(const float* U, const float* X, const float* C, co
  *   bf16 operand copies: "bf16_w", "bf16_x", "bf16_wt", "bf16_q", "bf16_p",
  *     "bf16_t";
  *   scans: "scan_fwd", "scan_bwd", "reduce_vb", and "proj_scan_fwd" (the
- *     fused projection + scan of inference).
+ *     fused projection + scan of inference);
+ *   vocabulary rows: "logprobs", "distill" (and "logprobs_join",
+ *     "distill_join" where a row is cut into parts), "logprobs_grad",
+ *     "distill_grad".
  * The caller owns the events and reads them after synchronising.
  * Disarmed (the default), launches record nothing.
  * ------------------------------------------------------------------------- */

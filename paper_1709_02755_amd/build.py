@@ -87,17 +87,20 @@ def build_sanitized(verbose: bool = False) -> str:
     if not all(os.path.exists(os.path.join(OBJDIR, os.path.basename(p) + ".o"))
                for p in glob.glob(os.path.join(CSRC, "*.hip"))):
         build()
-    api = os.path.join(CSRC, "sru_api.hip")
-    obj = os.path.join(OBJDIR, "sru_api.sanitized.o")
+    apis = [os.path.join(CSRC, n) for n in ("sru_api.hip", "sru_lm_api.hip")]
     flags = [f if f != "-O3" else "-O1" for f in HIP_FLAGS] + ["-g"]
-    cmd = [hipcc(), "-x", "hip", "-c", api, "-o", obj] + flags + SAN_FLAGS
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"sanitized compile failed:\n{r.stdout}\n{r.stderr}")
+    sanitized = []
+    for api in apis:
+        obj = os.path.join(OBJDIR, os.path.basename(api) + ".sanitized.o")
+        cmd = [hipcc(), "-x", "hip", "-c", api, "-o", obj] + flags + SAN_FLAGS
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"sanitized compile failed:\n{r.stdout}\n{r.stderr}")
+        sanitized.append(obj)
     others = [os.path.join(OBJDIR, os.path.basename(p) + ".o")
-              for p in sorted(glob.glob(os.path.join(CSRC, "*.hip"))) if p != api]
+              for p in sorted(glob.glob(os.path.join(CSRC, "*.hip"))) if p not in apis]
     cmd = ([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-shared-libsan", "-o",
-            SAN_LIB, obj] + others + SAN_FLAGS)
+            SAN_LIB] + sanitized + others + SAN_FLAGS)
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"sanitized link failed:\n{r.stdout}\n{r.stderr}")

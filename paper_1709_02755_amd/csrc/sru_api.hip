@@ -109,11 +109,7 @@ sru::ScanShape scan_shape(const Dims& s, int direction, const Opts& op = Opts())
 // v_f, v_r (and dv_f, dv_r) are required by the gated recurrence only
 bool missing_v(const Opts& op, const void* a, const void* b) { return !op.linear && (!a || !b); }
 
-int hip_status(hipError_t e) {
-  if (e == hipSuccess) return SRU_OK;
-  g_last_hip_error = (int)e;
-  return SRU_E_HIP;
-}
+using sru::hip_status;
 
 sru::GemmDesc gemm_desc(int op, bool bf16, int M, int N, int K, const void* A, long long lda,
                         const void* B, long long ldb, float* C, long long ldc) {
@@ -402,6 +398,12 @@ int scratch_on_current_device(void** out) {
 
 namespace sru {
 
+int hip_status(hipError_t e) {
+  if (e == hipSuccess) return SRU_OK;
+  g_last_hip_error = (int)e;
+  return SRU_E_HIP;
+}
+
 void timing_before(const char* label, hipStream_t stream) {
   TimingState& t = g_timing;
   if (!t.events || t.used + 2 > t.capacity) return;
@@ -456,7 +458,7 @@ const char* sru_status_string(int status) {
 
 int sru_last_hip_error(void) { return g_last_hip_error; }
 
-int sru_version(void) { return (1 << 16) | 4; }
+int sru_version(void) { return (1 << 16) | 5; }
 
 size_t sru_forward_workspace_bytes(int L, int B, int d_in, int d, int direction, int gemm_dtype) {
   Dims s;

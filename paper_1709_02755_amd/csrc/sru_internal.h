@@ -261,4 +261,7 @@ VbSum scan_backward_vb(const ScanShape& s, const ScanBwdArgs& a);
 void timing_before(const char* label, hipStream_t stream);
 void timing_after(hipStream_t stream);
 
+// hipError_t -> sru_status; a failure is kept for sru_last_hip_error().
+int hip_status(hipError_t e);
+
 }  // namespace sru

@@ -1,0 +1,208 @@
+// C ABI of the language model operators: argument validation, workspace sizes
+// and dispatch.  Every check runs before anything is enqueued; nothing here
+// allocates, frees or synchronises.
+#include <limits.h>
+
+#include <cmath>
+
+#include <initializer_list>
+
+#include "../../include/sru.h"
+#include "sru_lm.h"
+
+namespace {
+
+using sru::hip_status;
+
+constexpr long long kMaxElems = 1LL << 40;  // per tensor, far beyond any HBM size
+
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+bool valid_dtype(int t) { return t == SRU_DTYPE_FP32 || t == SRU_DTYPE_BF16; }
+size_t elem_size(int t) { return t == SRU_DTYPE_BF16 ? 2 : 4; }
+size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+
+bool any_null(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if (!p) return true;
+  return false;
+}
+bool all_aligned(std::initializer_list<const void*> ptrs, size_t n) {
+  for (const void* p : ptrs)
+    if (!aligned(p, n)) return false;
+  return true;
+}
+
+int check_workspace(size_t need, const void* workspace, size_t bytes) {
+  if (need == 0) return SRU_OK;
+  if (!workspace || bytes < need) return SRU_E_WORKSPACE;
+  return aligned(workspace, 256) ? SRU_OK : SRU_E_ALIGN;
+}
+
+// Vocabulary rows: shared checks of the logits' sizes, type and temperature.
+int check_rows(const void* z, long long ld, int dtype, int N, int V, float temperature,
+               sru::VocabRows& r) {
+  if (!valid_dtype(dtype)) return SRU_E_FLAG;
+  // a column past a row's end is told by its sign
+  if (N <= 0 || V <= 0 || V > INT_MAX / 2 || ld < V || ld > kMaxElems / N) return SRU_E_SHAPE;
+  if (!std::isfinite(temperature) || !(temperature > 0.f) || !std::isfinite(1.f / temperature))
+    return SRU_E_SHAPE;
+  if (!z) return SRU_E_NULLPTR;
+  if (!aligned(z, elem_size(dtype))) return SRU_E_ALIGN;
+  r = sru::VocabRows{z, ld, dtype == SRU_DTYPE_BF16, N, V, temperature};
+  return SRU_OK;
+}
+
+int check_grad(const void* dz, long long ldd, int dtype, int N, int V) {
+  if (ldd < V || ldd > kMaxElems / N) return SRU_E_SHAPE;
+  if (!dz) return SRU_E_NULLPTR;
+  return aligned(dz, elem_size(dtype)) ? SRU_OK : SRU_E_ALIGN;
+}
+
+int check_teacher(const int64_t* ids, const void* logits, int dtype, int N, int K) {
+  if (!valid_dtype(dtype)) return SRU_E_FLAG;
+  if (K <= 0 || K > SRU_MAX_TEACHER) return SRU_E_SHAPE;
+  if (!ids || !logits) return SRU_E_NULLPTR;
+  return aligned(ids, 8) && aligned(logits, elem_size(dtype)) ? SRU_OK : SRU_E_ALIGN;
+}
+
+}  // namespace
+
+static_assert(SRU_MAX_TOP == sru::kMaxTop && SRU_MAX_TEACHER == sru::kMaxTeacher, "limits");
+
+extern "C" {
+
+size_t sru_token_logprobs_workspace_bytes(int N, int V, int dtype, int top) {
+  if (N <= 0 || V <= 0 || !valid_dtype(dtype) || top < 0 || top > SRU_MAX_TOP) return 0;
+  return align_up(sru::logprob_workspace_bytes(N, V, dtype == SRU_DTYPE_BF16, top));
+}
+
+int sru_token_logprobs(const void* logits, long long ld, int dtype, const int64_t* tokens, int N,
+                       int V, int top, float temperature, float* logprob, float* entropy,
+                       float* stats, int64_t* top_ids, float* top_logprobs, void* workspace,
+                       size_t workspace_bytes, hipStream_t stream) {
+  sru::LogprobArgs a{};
+  if (int e = check_rows(logits, ld, dtype, N, V, temperature, a.r)) return e;
+  if (top < 0 || top > SRU_MAX_TOP || top > V) return SRU_E_SHAPE;
+  if (any_null({tokens, logprob, entropy, stats})) return SRU_E_NULLPTR;
+  if (top > 0 && any_null({top_ids, top_logprobs})) return SRU_E_NULLPTR;
+  if (!all_aligned({tokens, top_ids}, 8) ||
+      !all_aligned({logprob, entropy, stats, top_logprobs}, 4))
+    return SRU_E_ALIGN;
+  const size_t need = sru_token_logprobs_workspace_bytes(N, V, dtype, top);
+  if (int e = check_workspace(need, workspace, workspace_bytes)) return e;
+  a.tokens = tokens;
+  a.top = top;
+  a.logprob = logprob;
+  a.entropy = entropy;
+  a.stats = stats;
+  a.top_ids = top_ids;
+  a.top_logprobs = top_logprobs;
+  a.workspace = workspace;
+  return hip_status(sru::logprob_launch(a, stream));
+}
+
+int sru_token_logprobs_backward(const void* logits, long long ld, int dtype,
+                                const int64_t* tokens, const float* stats, const float* entropy,
+                                const float* dlogprob, const float* dentropy,
+                                const int64_t* top_ids, const float* dtop, int N, int V, int top,
+                                float temperature, void* dlogits, long long ldd,
+                                hipStream_t stream) {
+  sru::LogprobGradArgs a{};
+  if (int e = check_rows(logits, ld, dtype, N, V, temperature, a.r)) return e;
+  if (top < 0 || top > SRU_MAX_TOP || top > V || (dtop && top == 0)) return SRU_E_SHAPE;
+  if (int e = check_grad(dlogits, ldd, dtype, N, V)) return e;
+  if (any_null({tokens, stats}) || (dentropy && !entropy) || (dtop && !top_ids))
+    return SRU_E_NULLPTR;
+  if (!all_aligned({tokens, top_ids}, 8) ||
+      !all_aligned({stats, entropy, dlogprob, dentropy, dtop}, 4))
+    return SRU_E_ALIGN;
+  a.tokens = tokens;
+  a.stats = stats;
+  a.entropy = entropy;
+  a.dlogprob = dlogprob;
+  a.dentropy = dentropy;
+  a.top_ids = top_ids;
+  a.dtop = dtop;
+  a.top = top;
+  a.dz = dlogits;
+  a.ldd = ldd;
+  return hip_status(sru::logprob_grad_launch(a, stream));
+}
+
+size_t sru_distill_workspace_bytes(int N, int V, int dtype) {
+  if (N <= 0 || V <= 0 || !valid_dtype(dtype)) return 0;
+  return align_up(sru::distill_workspace_bytes(N, V, dtype == SRU_DTYPE_BF16));
+}
+
+int sru_distill_forward(const void* logits, long long ld, int dtype, const int64_t* teacher_ids,
+                        const void* teacher_logits, int teacher_dtype, int N, int V, int K,
+                        float temperature, float* loss, float* stats, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream) {
+  sru::DistillArgs a{};
+  if (int e = check_rows(logits, ld, dtype, N, V, temperature, a.r)) return e;
+  if (int e = check_teacher(teacher_ids, teacher_logits, teacher_dtype, N, K)) return e;
+  if (any_null({loss, stats})) return SRU_E_NULLPTR;
+  if (!all_aligned({loss, stats}, 4)) return SRU_E_ALIGN;
+  if (int e = check_workspace(sru_distill_workspace_bytes(N, V, dtype), workspace,
+                              workspace_bytes))
+    return e;
+  a.ids = teacher_ids;
+  a.teacher = teacher_logits;
+  a.teacher_bf16 = teacher_dtype == SRU_DTYPE_BF16;
+  a.K = K;
+  a.loss = loss;
+  a.stats = stats;
+  a.workspace = workspace;
+  return hip_status(sru::distill_launch(a, stream));
+}
+
+int sru_distill_backward(const void* logits, long long ld, int dtype, const int64_t* teacher_ids,
+                         const void* teacher_logits, int teacher_dtype, const float* stats,
+                         const float* dloss, int N, int V, int K, float temperature,
+                         void* dlogits, long long ldd, hipStream_t stream) {
+  sru::DistillArgs a{};
+  if (int e = check_rows(logits, ld, dtype, N, V, temperature, a.r)) return e;
+  if (int e = check_teacher(teacher_ids, teacher_logits, teacher_dtype, N, K)) return e;
+  if (int e = check_grad(dlogits, ldd, dtype, N, V)) return e;
+  if (any_null({stats, dloss})) return SRU_E_NULLPTR;
+  if (!all_aligned({stats, dloss}, 4)) return SRU_E_ALIGN;
+  a.ids = teacher_ids;
+  a.teacher = teacher_logits;
+  a.teacher_bf16 = teacher_dtype == SRU_DTYPE_BF16;
+  a.K = K;
+  a.dloss = dloss;
+  a.stats = const_cast<float*>(stats);  // read only where loss is NULL
+  a.dz = dlogits;
+  a.ldd = ldd;
+  return hip_status(sru::distill_launch(a, stream));
+}
+
+int sru_distill_forward_backward(const void* logits, long long ld, int dtype,
+                                 const int64_t* teacher_ids, const void* teacher_logits,
+                                 int teacher_dtype, const float* dloss, int N, int V, int K,
+                                 float temperature, float* loss, float* stats, void* dlogits,
+                                 long long ldd, void* workspace, size_t workspace_bytes,
+                                 hipStream_t stream) {
+  sru::DistillArgs a{};
+  if (int e = check_rows(logits, ld, dtype, N, V, temperature, a.r)) return e;
+  if (int e = check_teacher(teacher_ids, teacher_logits, teacher_dtype, N, K)) return e;
+  if (int e = check_grad(dlogits, ldd, dtype, N, V)) return e;
+  if (any_null({dloss, loss, stats})) return SRU_E_NULLPTR;
+  if (!all_aligned({dloss, loss, stats}, 4)) return SRU_E_ALIGN;
+  if (int e = check_workspace(sru_distill_workspace_bytes(N, V, dtype), workspace,
+                              workspace_bytes))
+    return e;
+  a.ids = teacher_ids;
+  a.teacher = teacher_logits;
+  a.teacher_bf16 = teacher_dtype == SRU_DTYPE_BF16;
+  a.K = K;
+  a.dloss = dloss;
+  a.loss = loss;
+  a.stats = stats;
+  a.dz = dlogits;
+  a.ldd = ldd;
+  a.workspace = workspace;
+  return hip_status(sru::distill_launch(a, stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,847 @@
+// Rows of logits over a vocabulary: log probabilities of given tokens with
+// entropy and top alternatives, distillation from a teacher's top logits, and
+// their gradients.
+//
+// All of them need, of a row z of V logits at temperature T,
+//   m = max z,  S = sum_j e^{x_j},  x_j = (z_j - m) / T  (and sum_j e^{x_j} x_j),
+// taken in one pass with a running maximum, and then elementwise work.  They
+// are bound by reading (and writing) the rows.
+#include <math.h>
+
+#include "sru_lm.h"
+
+namespace sru {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.693147180559945309f;
+// 2^x is 0 in fp32 from here down: exponents are cut here where they are a
+// factor, so that a probability of 0 times its log is 0 and not NaN (logits
+// of -inf, or of the type's lowest value at a temperature below 1).
+constexpr float kLowExp = -200.0f;
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <bool BF16>
+struct Elem;
+template <>
+struct Elem<false> {
+  using T = float;
+  static constexpr int VE = 4;  // elements of a 16-byte vector
+  static __device__ __forceinline__ float get(float v) { return v; }
+  static __device__ __forceinline__ float put(float v) { return v; }
+  static __device__ __forceinline__ void unpack(const uint4& u, float (&f)[4]) {
+    f[0] = __uint_as_float(u.x);
+    f[1] = __uint_as_float(u.y);
+    f[2] = __uint_as_float(u.z);
+    f[3] = __uint_as_float(u.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                      __float_as_uint(f[3]));
+  }
+  static constexpr unsigned kNegInf = 0xff800000u;
+};
+template <>
+struct Elem<true> {
+  using T = uint16_t;
+  static constexpr int VE = 8;
+  static __device__ __forceinline__ float get(uint16_t v) {
+    return __uint_as_float((unsigned)v << 16);
+  }
+  static __device__ __forceinline__ uint16_t put(float v) {
+    return __builtin_bit_cast(uint16_t, (__bf16)v);
+  }
+  static __device__ __forceinline__ void unpack(const uint4& u, float (&f)[8]) {
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (unsigned)put(f[2 * i]) | ((unsigned)put(f[2 * i + 1]) << 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static constexpr unsigned kNegInf = 0xff80ff80u;
+};
+
+// How a row is cut: up to the first 16-byte boundary, whole vectors, the rest.
+// A part of a row is a range of its vectors; the first part takes the head
+// and the last one the tail as well.
+struct Span {
+  int head, nvec, tail;
+};
+template <bool BF16>
+__device__ __forceinline__ Span row_span(const typename Elem<BF16>::T* z, int V) {
+  constexpr int ES = sizeof(typename Elem<BF16>::T), VE = Elem<BF16>::VE;
+  const int mis = (int)(reinterpret_cast<uintptr_t>(z) & 15);
+  Span s;
+  s.head = min(V, ((16 - mis) & 15) / ES);
+  s.nvec = (V - s.head) / VE;
+  s.tail = s.head + s.nvec * VE;
+  return s;
+}
+
+// ------------------------------------------------------- running statistics
+// Maximum m, s = sum 2^x and t = sum 2^x x with x = (z - m) k, k = log2(e) / T.
+// base is m, or 0 while there is nothing above -inf (z - base is then -inf and
+// adds 0, where z - m would be NaN).  A NaN or +inf makes s NaN.
+template <bool ENT>
+struct Run {
+  float m = -INFINITY, base = 0.f, s = 0.f, t = 0.f;
+
+  // brings (s, t) to the maximum nm >= m
+  __device__ __forceinline__ void to(float nm, float k) {
+    // m = -inf: nothing was added, and nothing is scaled
+    const float d = m == -INFINITY ? 0.f : fmaxf((m - nm) * k, kLowExp);
+    const float f = m == nm ? 1.f : exp2_hw(d);
+    if constexpr (ENT) t = m == nm ? t : f * (t + d * s);
+    s *= f;
+    m = nm;
+    base = nm == -INFINITY ? 0.f : nm;
+  }
+  template <int VE>
+  __device__ __forceinline__ void add(const float (&z)[VE], float vmax, float k) {
+    if (vmax > m) to(vmax, k);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      const float x = (z[j] - base) * k;
+      const float e = exp2_hw(x);
+      s += e;
+      if constexpr (ENT) t = fmaf(e, fmaxf(x, kLowExp), t);
+    }
+  }
+  __device__ __forceinline__ void join(const Run& o, float k) {
+    Run a = *this, b = o;
+    const float nm = fmaxf(a.m, b.m);
+    a.to(nm, k);
+    b.to(nm, k);
+    *this = a;
+    s += b.s;
+    if constexpr (ENT) t += b.t;
+  }
+};
+
+template <bool ENT>
+__device__ __forceinline__ void run_store(float* p, const Run<ENT>& r) {
+  p[0] = r.m;
+  p[1] = r.s;
+  p[2] = r.t;
+}
+template <bool ENT>
+__device__ __forceinline__ Run<ENT> run_load(const float* p) {
+  Run<ENT> r;
+  r.m = p[0];
+  r.base = r.m == -INFINITY ? 0.f : r.m;
+  r.s = p[1];
+  r.t = p[2];
+  return r;
+}
+
+// The statistics of a workgroup's threads, the same in every thread; always in
+// the same order.  lds: 3 floats a wave; barriers inside.
+template <int THREADS, bool ENT>
+__device__ __forceinline__ Run<ENT> run_block(Run<ENT> r, float k, float* lds) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    Run<ENT> b;
+    b.m = __shfl_xor(r.m, o);
+    b.s = __shfl_xor(r.s, o);
+    if constexpr (ENT) b.t = __shfl_xor(r.t, o);
+    r.join(b, k);
+  }
+  constexpr int W = THREADS / 64;
+  if ((threadIdx.x & 63) == 0) run_store(lds + 3 * (threadIdx.x >> 6), r);
+  __syncthreads();
+  r = run_load<ENT>(lds);
+#pragma unroll
+  for (int w = 1; w < W; ++w) r.join(run_load<ENT>(lds + 3 * w), k);
+  __syncthreads();
+  return r;
+}
+
+// ---------------------------------------------------------- top alternatives
+// Values are ordered by an unsigned key (larger = better), equal ones by the
+// lower column; -0 counts as 0, and a NaN is no alternative.
+__device__ __forceinline__ unsigned top_key(float z) {
+  const unsigned u = __float_as_uint(z + 0.0f);
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float top_value(unsigned key) {
+  return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ bool top_better(unsigned k, unsigned i, unsigned k2, unsigned i2) {
+  return k > k2 || (k == k2 && i < i2);
+}
+
+// A wave's best K: lane l holds the l-th.  Empty places have key 0, below that
+// of any number.
+struct TopList {
+  unsigned key = 0, idx = 0xffffffffu;  // this lane's entry
+  unsigned tk = 0, ti = 0xffffffffu;    // the K-th, uniform
+  __device__ __forceinline__ void insert(unsigned k, unsigned i, int K) {
+    const int pos = __popcll(__ballot(top_better(key, idx, k, i)));
+    const int lane = threadIdx.x & 63;
+    const unsigned pk = __shfl_up(key, 1), pi = __shfl_up(idx, 1);
+    if (lane > pos) {
+      key = pk;
+      idx = pi;
+    } else if (lane == pos) {
+      key = k;
+      idx = i;
+    }
+    tk = __builtin_amdgcn_readlane(key, K - 1);
+    ti = __builtin_amdgcn_readlane(idx, K - 1);
+  }
+  // Candidates of the wave's lanes, one each where ok: whatever the others do
+  // to the list, each better one than its K-th goes in.
+  __device__ __forceinline__ void offer(bool ok, unsigned k, unsigned i, int K) {
+    while (true) {
+      const unsigned long long b = __ballot(ok && top_better(k, i, tk, ti));
+      if (!b) break;
+      const int src = __ffsll((long long)b) - 1;
+      insert(__builtin_amdgcn_readlane(k, src), __builtin_amdgcn_readlane(i, src), K);
+      ok = ok && (int)(threadIdx.x & 63) != src;
+    }
+  }
+};
+
+// -------------------------------------------------------------- one row part
+// Statistics (and the wave's best alternatives) of a part of a row.  `floor`
+// (LDS, one word, 0 before) holds the best K-th key that any wave has: K
+// values are at least that good, so nothing below it is looked at.
+template <bool BF16, int THREADS, int U, bool ENT, bool TOP>
+__device__ __forceinline__ Run<ENT> part_stats(const typename Elem<BF16>::T* z, int V, int part,
+                                               int parts, float k, int K, unsigned* floor,
+                                               TopList& top) {
+  using E = Elem<BF16>;
+  constexpr int VE = E::VE;
+  const Span sp = row_span<BF16>(z, V);
+  const int tid = threadIdx.x;
+  const int v0 = (int)((long long)sp.nvec * part / parts);
+  const int v1 = (int)((long long)sp.nvec * (part + 1) / parts);
+  const uint4* zv = reinterpret_cast<const uint4*>(z + sp.head);
+  Run<ENT> run;
+
+  auto take = [&](const float(&f)[VE], unsigned col) {
+    float vm = f[0];
+#pragma unroll
+    for (int j = 1; j < VE; ++j) vm = fmaxf(vm, f[j]);
+    run.add(f, vm, k);
+    if constexpr (TOP) {
+      const unsigned shared = *(volatile unsigned*)floor;
+      if (__any(top_key(vm) >= max(top.tk, shared))) {
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+          const unsigned key = top_key(f[j]);
+          // places past the part's end are -inf with a column that is none
+          top.offer(f[j] == f[j] && key >= shared && col + j < (unsigned)V, key, col + j, K);
+        }
+        if (top.tk > shared && (tid & 63) == 0) atomicMax(floor, top.tk);
+      }
+    }
+  };
+
+  for (int v = v0; v < v1; v += THREADS * U) {
+    uint4 u[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int at = v + i * THREADS + tid;
+      u[i] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
+      if (at < v1) u[i] = zv[at];
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int at = v + i * THREADS + tid;
+      float f[VE];
+      E::unpack(u[i], f);
+      take(f, at < v1 ? (unsigned)(sp.head + at * VE) : 0x80000000u);
+    }
+  }
+  // the head and the tail, at most VE - 1 elements each, one a lane
+  int col = -1;
+  if (part == 0 && tid < sp.head) col = tid;
+  if (part == parts - 1 && tid >= 32 && tid - 32 < V - sp.tail) col = sp.tail + tid - 32;
+  if (tid < 64) {
+    float f[VE];
+#pragma unroll
+    for (int j = 0; j < VE; ++j) f[j] = -INFINITY;
+    if (col >= 0) f[0] = E::get(z[col]);
+    float vm = f[0];
+    run.add(f, vm, k);
+    if constexpr (TOP)
+      top.offer(col >= 0 && vm == vm && top_key(vm) >= *(volatile unsigned*)floor, top_key(vm),
+                (unsigned)col, K);
+  }
+  return run;
+}
+
+// The best K of n lists of K (key, column) pairs each, best first, in LDS:
+// every entry's rank is the number of entries that are better, found in each
+// other list by halving.  put(rank, key, column) for the K best.
+template <int THREADS, typename F>
+__device__ __forceinline__ void top_merge(const uint2* lists, int n, int K, F put) {
+  for (int e = threadIdx.x; e < n * K; e += THREADS) {
+    const uint2 x = lists[e];
+    const int mine = e / K;
+    int rank = e - mine * K;
+    for (int l = 0; l < n && rank < K; ++l) {
+      if (l == mine) continue;
+      int lo = 0, hi = K;  // entries before lo are better than x
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        const uint2 y = lists[l * K + mid];
+        // empty places are all alike: those of earlier lists come first
+        const bool better = top_better(y.x, y.y, x.x, x.y) ||
+                            (y.x == x.x && y.y == x.y && l < mine);
+        if (better) lo = mid + 1;
+        else hi = mid;
+      }
+      rank += lo;
+    }
+    if (rank < K) put(rank, x.x, x.y);
+  }
+}
+
+struct RowStats {
+  float m, base, s, log_s;
+};
+__device__ __forceinline__ RowStats row_stats(float m, float s) {
+  return RowStats{m, m == -INFINITY ? 0.f : m, s, logf(s)};
+}
+// log probability of a logit; a row with no logit above -inf gives -inf
+__device__ __forceinline__ float row_logprob(const RowStats& r, float z, float inv_t) {
+  return r.s == 0.f ? -INFINITY : (z - r.base) * inv_t - r.log_s;
+}
+
+// ------------------------------------------------- token log probabilities
+template <bool BF16>
+__device__ __forceinline__ void logprob_write(const LogprobArgs& a, int row, float m, float s,
+                                              float t, float inv_t) {
+  using E = Elem<BF16>;
+  const RowStats st = row_stats(m, s);
+  a.stats[2LL * row] = m;
+  a.stats[2LL * row + 1] = s;
+  // H = log S - sum e^x x / S (t is in units of log 2); 0 where nothing is possible
+  a.entropy[row] = s == 0.f ? 0.f : st.log_s - kLn2 * t / s;
+  const int64_t tok = a.tokens[row];
+  float lp = 0.f;
+  if (tok >= 0 && tok < a.r.V) {
+    const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
+    lp = row_logprob(st, E::get(z[tok]), inv_t);
+  }
+  a.logprob[row] = lp;
+}
+
+__device__ __forceinline__ void top_write(const LogprobArgs& a, int row, const RowStats& st,
+                                          float inv_t, int rank, unsigned key, unsigned idx) {
+  const long long o = (long long)row * a.top + rank;
+  a.top_ids[o] = key ? (int64_t)idx : -1;
+  a.top_logprobs[o] = key ? row_logprob(st, top_value(key), inv_t) : -INFINITY;
+}
+
+// One part of one row per workgroup.  parts == 1: the row's results; else its
+// statistics and its best alternatives go to the workspace, [row, part] of 4
+// floats, then [row, part, K] pairs.
+template <bool BF16, int THREADS, int U, bool TOP>
+__global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a, int parts) {
+  constexpr int W = THREADS / 64;
+  __shared__ float red[3 * W];
+  __shared__ unsigned floor;
+  __shared__ uint2 lists[TOP ? W * kMaxTop : 1];
+  using E = Elem<BF16>;
+  const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
+  const long long items = (long long)a.r.N * parts;
+  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+    const int row = (int)(it / parts), part = (int)(it - (long long)row * parts);
+    const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
+    TopList top;
+    if constexpr (TOP) {
+      if (threadIdx.x == 0) floor = 0;
+      __syncthreads();
+    }
+    Run<true> run = part_stats<BF16, THREADS, U, true, TOP>(z, a.r.V, part, parts, k, a.top,
+                                                            &floor, top);
+    if constexpr (TOP) {
+      const int lane = threadIdx.x & 63;
+      if (lane < a.top) lists[(threadIdx.x >> 6) * a.top + lane] = make_uint2(top.key, top.idx);
+    }
+    run = run_block<THREADS>(run, k, red);  // its barriers make the lists visible
+    if (parts == 1) {
+      if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
+      if constexpr (TOP) {
+        const RowStats st = row_stats(run.m, run.s);
+        top_merge<THREADS>(lists, W, a.top, [&](int rank, unsigned key, unsigned idx) {
+          top_write(a, row, st, inv_t, rank, key, idx);
+        });
+      }
+    } else {
+      float* ws = static_cast<float*>(a.workspace);
+      if (threadIdx.x == 0) run_store(ws + 4 * it, run);
+      if constexpr (TOP) {
+        uint2* wl = reinterpret_cast<uint2*>(ws + 4 * items) + it * a.top;
+        top_merge<THREADS>(lists, W, a.top, [&](int rank, unsigned key, unsigned idx) {
+          wl[rank] = make_uint2(key, idx);
+        });
+      }
+    }
+    __syncthreads();  // lists and floor are used again
+  }
+}
+
+constexpr int kMaxParts = 64;
+
+// The parts of a row joined, one workgroup per row.
+template <bool BF16, bool TOP>
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int parts) {
+  extern __shared__ uint2 lists[];
+  const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
+  const float* ws = static_cast<const float*>(a.workspace);
+  const uint2* wl = reinterpret_cast<const uint2*>(ws + 4LL * a.r.N * parts);
+  for (int row = blockIdx.x; row < a.r.N; row += gridDim.x) {
+    if constexpr (TOP) {
+      for (int e = threadIdx.x; e < parts * a.top; e += 256)
+        lists[e] = wl[(long long)row * parts * a.top + e];
+    }
+    // one part a lane, joined across the wave; every wave does the same
+    const int lane = threadIdx.x & 63;
+    Run<true> run;
+    if (lane < parts) run = run_load<true>(ws + 4 * ((long long)row * parts + lane));
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      Run<true> b;
+      b.m = __shfl_xor(run.m, o);
+      b.s = __shfl_xor(run.s, o);
+      b.t = __shfl_xor(run.t, o);
+      run.join(b, k);
+    }
+    if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
+    if constexpr (TOP) {
+      __syncthreads();
+      const RowStats st = row_stats(run.m, run.s);
+      top_merge<256>(lists, parts, a.top, [&](int rank, unsigned key, unsigned idx) {
+        top_write(a, row, st, inv_t, rank, key, idx);
+      });
+      __syncthreads();
+    }
+  }
+}
+
+// ------------------------------------------------------------------ gradients
+// dz_j = e_j (c0 + c1 x_j), e_j = 2^{x_j}, over a part of a row.
+template <bool BF16, int THREADS, int U, bool LIN>
+__device__ __forceinline__ void part_grad(const typename Elem<BF16>::T* z,
+                                          typename Elem<BF16>::T* dz, int V, int part, int parts,
+                                          float base, float k, float c0, float c1) {
+  using E = Elem<BF16>;
+  constexpr int VE = E::VE;
+  const Span sp = row_span<BF16>(z, V);
+  const int tid = threadIdx.x;
+  const int v0 = (int)((long long)sp.nvec * part / parts);
+  const int v1 = (int)((long long)sp.nvec * (part + 1) / parts);
+  const uint4* zv = reinterpret_cast<const uint4*>(z + sp.head);
+  uint4* dv = reinterpret_cast<uint4*>(dz + sp.head);
+  // rows of another alignment than their logits' are written element by element
+  const bool whole = ((reinterpret_cast<uintptr_t>(dv)) & 15) == 0;
+  // a row that adds nothing: exact zeros, whatever its logits are
+  const bool none = c0 == 0.f && c1 == 0.f;
+  auto grad = [&](float zj) {
+    const float x = (zj - base) * k;
+    const float e = exp2_hw(x);
+    return none ? 0.f : LIN ? e * fmaf(c1, fmaxf(x, kLowExp), c0) : e * c0;
+  };
+  for (int v = v0; v < v1; v += THREADS * U) {
+    uint4 u[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int at = v + i * THREADS + tid;
+      if (at < v1 && !none) u[i] = zv[at];
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int at = v + i * THREADS + tid;
+      if (at < v1) {
+        float f[VE];
+        E::unpack(u[i], f);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) f[j] = grad(f[j]);
+        if (whole) {
+          dv[at] = E::pack(f);
+        } else {
+#pragma unroll
+          for (int j = 0; j < VE; ++j) dz[sp.head + at * VE + j] = E::put(f[j]);
+        }
+      }
+    }
+  }
+  if (part == 0 && tid < sp.head) dz[tid] = E::put(grad(E::get(z[tid])));
+  if (part == parts - 1 && tid < V - sp.tail)
+    dz[sp.tail + tid] = E::put(grad(E::get(z[sp.tail + tid])));
+}
+
+// Whether column col lies in this part of the row.
+template <bool BF16>
+__device__ __forceinline__ bool in_part(const typename Elem<BF16>::T* z, int V, int col, int part,
+                                        int parts) {
+  constexpr int VE = Elem<BF16>::VE;
+  const Span sp = row_span<BF16>(z, V);
+  if (col < sp.head) return part == 0;
+  if (col >= sp.tail) return part == parts - 1;
+  const int v = (col - sp.head) / VE;
+  const int v0 = (int)((long long)sp.nvec * part / parts);
+  const int v1 = (int)((long long)sp.nvec * (part + 1) / parts);
+  return v >= v0 && v < v1;
+}
+
+// The columns with a term of their own: n (column, weight) pairs in LDS,
+// column -1 = none.  Entry e of the n belongs to thread e % THREADS; where a
+// column occurs more than once its first entry adds all of them.  Before the
+// part's gradient is written, each owner takes its logit; dz may be z.
+template <bool BF16, int THREADS, int MAXN, bool LIN>
+struct PointTerms {
+  static constexpr int PER = (MAXN + THREADS - 1) / THREADS;
+  using E = Elem<BF16>;
+  float value[PER];
+  int at[PER];
+  __device__ __forceinline__ void take(const int* cols, const float* w, int n,
+                                       const typename E::T* z, int V, int part, int parts,
+                                       float base, float k, float c0, float c1) {
+    const bool none = c0 == 0.f && c1 == 0.f;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int e = p * THREADS + (int)threadIdx.x;
+      at[p] = -1;
+      if (e >= n) continue;
+      const int c = cols[e];
+      if (c < 0 || !in_part<BF16>(z, V, c, part, parts)) continue;
+      float sum = 0.f;
+      int first = e;
+      for (int q = 0; q < n; ++q)
+        if (cols[q] == c) {
+          first = min(first, q);
+          sum += w[q];
+        }
+      if (first != e) continue;
+      const float x = (E::get(z[c]) - base) * k;
+      const float g = none ? 0.f
+                           : exp2_hw(x) * (LIN ? fmaf(c1, fmaxf(x, kLowExp), c0) : c0);
+      value[p] = g + sum;
+      at[p] = c;
+    }
+  }
+  __device__ __forceinline__ void put(typename E::T* dz) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+      if (at[p] >= 0) dz[at[p]] = E::put(value[p]);
+  }
+};
+
+// dz_j = (1/T) (w_t [j = t] + sum_k w_k [j = id_k] - p_j A - dH p_j (log p_j + H)),
+// A = w_t + sum_k w_k, with p = e / S and log p = x ln2 - log S.
+template <bool BF16, int THREADS, int U>
+__global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LogprobGradArgs a, int parts) {
+  using E = Elem<BF16>;
+  __shared__ int cols[kMaxTop + 1];
+  __shared__ float wts[kMaxTop + 1];
+  const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
+  const int n = 1 + (a.dtop ? a.top : 0);
+  const long long items = (long long)a.r.N * parts;
+  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+    const int row = (int)(it / parts), part = (int)(it - (long long)row * parts);
+    const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
+    auto* dz = static_cast<typename E::T*>(a.dz) + (long long)row * a.ldd;
+    const float s = a.stats[2LL * row + 1];
+    const RowStats st = row_stats(a.stats[2LL * row], s);
+    for (int e = threadIdx.x; e < n; e += THREADS) {
+      const int64_t c = e == 0 ? (a.dlogprob ? a.tokens[row] : -1)
+                               : a.top_ids[(long long)row * a.top + e - 1];
+      const bool live = c >= 0 && c < a.r.V && s != 0.f;
+      cols[e] = live ? (int)c : -1;
+      wts[e] = !live ? 0.f
+                     : inv_t * (e == 0 ? a.dlogprob[row] : a.dtop[(long long)row * a.top + e - 1]);
+    }
+    __syncthreads();
+    float sum = 0.f;
+    for (int e = 0; e < n; ++e) sum += wts[e];
+    const float inv_s = s == 0.f ? 0.f : 1.f / s;
+    const float dh = a.dentropy && s != 0.f ? a.dentropy[row] * inv_t : 0.f;
+    const float c0 = -(sum + (dh == 0.f ? 0.f : dh * (a.entropy[row] - st.log_s))) * inv_s;
+    const float c1 = dh == 0.f ? 0.f : -dh * kLn2 * inv_s;
+    PointTerms<BF16, THREADS, kMaxTop + 1, true> pt;
+    pt.take(cols, wts, n, z, a.r.V, part, parts, st.base, k, c0, c1);
+    __syncthreads();  // dz may be z
+    if (c1 == 0.f)
+      part_grad<BF16, THREADS, U, false>(z, dz, a.r.V, part, parts, st.base, k, c0, 0.f);
+    else
+      part_grad<BF16, THREADS, U, true>(z, dz, a.r.V, part, parts, st.base, k, c0, c1);
+    __syncthreads();
+    pt.put(dz);
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ distillation
+// The teacher's probabilities p = softmax(t / T) over the row's kept entries
+// (ids within the vocabulary, logits above -inf): cols[e], probs[e] in LDS;
+// returns 1 where there is any, else 0.  scratch: THREADS / 64 floats.
+template <int THREADS>
+__device__ __forceinline__ float teacher_probs(const DistillArgs& a, int row, int* cols,
+                                               float* probs, float* scratch, float k) {
+  constexpr int W = THREADS / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float m = -INFINITY;
+  for (int e = threadIdx.x; e < a.K; e += THREADS) {
+    const long long o = (long long)row * a.K + e;
+    const int64_t c = a.ids[o];
+    const float t = a.teacher_bf16 ? Elem<true>::get(static_cast<const uint16_t*>(a.teacher)[o])
+                                   : static_cast<const float*>(a.teacher)[o];
+    const bool kept = c >= 0 && c < a.r.V && t != -INFINITY;
+    cols[e] = kept ? (int)c : -1;
+    probs[e] = t;
+    // a NaN that fmaxf drops comes back in the sum
+    if (kept) m = fmaxf(m, t);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if (lane == 0) scratch[wave] = m;
+  __syncthreads();
+  for (int w = 0; w < W; ++w) m = fmaxf(m, scratch[w]);
+  __syncthreads();
+  float s = 0.f;
+  bool any = false;
+  for (int e = threadIdx.x; e < a.K; e += THREADS) {
+    const bool kept = cols[e] >= 0;
+    const float p = kept ? exp2_hw((probs[e] - m) * k) : 0.f;
+    probs[e] = p;
+    s += p;
+    any |= kept;
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
+  if (lane == 0) scratch[wave] = s;
+  const int rows_kept = __syncthreads_or(any);
+  s = 0.f;
+  for (int w = 0; w < W; ++w) s += scratch[w];
+  const float inv = 1.f / s;
+  for (int e = threadIdx.x; e < a.K; e += THREADS) probs[e] = cols[e] >= 0 ? probs[e] * inv : 0.f;
+  __syncthreads();
+  return rows_kept ? 1.f : 0.f;
+}
+
+// sum p (log p - log q) over the kept entries with p > 0, in every thread
+template <bool BF16, int THREADS>
+__device__ __forceinline__ float distill_loss(const DistillArgs& a, const int* cols,
+                                              const float* probs, float* scratch,
+                                              const typename Elem<BF16>::T* z, const RowStats& st,
+                                              float inv_t) {
+  constexpr int W = THREADS / 64;
+  float loss = 0.f;
+  for (int e = threadIdx.x; e < a.K; e += THREADS) {
+    const float p = probs[e];
+    // p = 0 (too small for fp32, or no entry) adds 0; a NaN stays one
+    if (p != 0.f) loss += p * (logf(p) - row_logprob(st, Elem<BF16>::get(z[cols[e]]), inv_t));
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) loss += __shfl_xor(loss, o);
+  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = loss;
+  __syncthreads();
+  loss = 0.f;
+  for (int w = 0; w < W; ++w) loss += scratch[w];
+  __syncthreads();
+  return loss;
+}
+
+// STATS: the row's statistics are taken here (else read); GRAD: its gradient
+// is written.  parts > 1 with STATS: only the part's statistics are, into the
+// workspace.
+template <bool BF16, int THREADS, int U, bool STATS, bool GRAD>
+__global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int parts) {
+  using E = Elem<BF16>;
+  constexpr int W = THREADS / 64;
+  __shared__ float red[3 * W];
+  __shared__ int cols[kMaxTeacher];
+  __shared__ float probs[kMaxTeacher];
+  const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
+  const long long items = (long long)a.r.N * parts;
+  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+    const int row = (int)(it / parts), part = (int)(it - (long long)row * parts);
+    const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
+    float m, s;
+    if constexpr (STATS) {
+      TopList none;
+      Run<false> run = part_stats<BF16, THREADS, U, false, false>(z, a.r.V, part, parts, k, 0,
+                                                                  nullptr, none);
+      run = run_block<THREADS>(run, k, red);
+      m = run.m;
+      s = run.s;
+      if (parts > 1) {
+        if (threadIdx.x == 0) run_store(static_cast<float*>(a.workspace) + 4 * it, run);
+        continue;
+      }
+    } else {
+      m = a.stats[2LL * row];
+      s = a.stats[2LL * row + 1];
+    }
+    const RowStats st = row_stats(m, s);
+    const float kept = teacher_probs<THREADS>(a, row, cols, probs, red, k);
+    if constexpr (STATS) {
+      const float loss = distill_loss<BF16, THREADS>(a, cols, probs, red, z, st, inv_t);
+      if (threadIdx.x == 0) {
+        a.loss[row] = loss;
+        a.stats[2LL * row] = m;
+        a.stats[2LL * row + 1] = s;
+      }
+    }
+    if constexpr (GRAD) {
+      auto* dz = static_cast<typename E::T*>(a.dz) + (long long)row * a.ldd;
+      // a row with no possible token, or no teacher, has no gradient
+      const float g = s == 0.f || kept == 0.f ? 0.f : a.dloss[row] * inv_t;
+      const float c0 = g == 0.f ? 0.f : g / s;
+      for (int e = threadIdx.x; e < a.K; e += THREADS) {
+        probs[e] = g == 0.f ? 0.f : -g * probs[e];
+        if (g == 0.f) cols[e] = -1;
+      }
+      __syncthreads();
+      PointTerms<BF16, THREADS, kMaxTeacher, false> pt;
+      pt.take(cols, probs, a.K, z, a.r.V, part, parts, st.base, k, c0, 0.f);
+      __syncthreads();  // dz may be z
+      part_grad<BF16, THREADS, U, false>(z, dz, a.r.V, part, parts, st.base, k, c0, 0.f);
+      __syncthreads();
+      pt.put(dz);
+    }
+    __syncthreads();
+  }
+}
+
+// The parts of a row joined, and its loss; one workgroup per row.
+template <bool BF16>
+__global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a, int parts) {
+  using E = Elem<BF16>;
+  __shared__ float red[4];
+  __shared__ int cols[kMaxTeacher];
+  __shared__ float probs[kMaxTeacher];
+  const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
+  const float* ws = static_cast<const float*>(a.workspace);
+  for (int row = blockIdx.x; row < a.r.N; row += gridDim.x) {
+    const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
+    const int lane = threadIdx.x & 63;
+    Run<false> run;
+    if (lane < parts) run = run_load<false>(ws + 4 * ((long long)row * parts + lane));
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      Run<false> b;
+      b.m = __shfl_xor(run.m, o);
+      b.s = __shfl_xor(run.s, o);
+      run.join(b, k);
+    }
+    const RowStats st = row_stats(run.m, run.s);
+    teacher_probs<256>(a, row, cols, probs, red, k);
+    const float loss = distill_loss<BF16, 256>(a, cols, probs, red, z, st, inv_t);
+    if (threadIdx.x == 0) {
+      a.loss[row] = loss;
+      a.stats[2LL * row] = run.m;
+      a.stats[2LL * row + 1] = run.s;
+    }
+    __syncthreads();
+  }
+}
+
+constexpr int kThreads = 512;
+constexpr int kUnroll = 4;
+
+// Parts a row is cut into: with fewer rows than CUs some would have nothing to
+// do, but a part has at least one round of vectors.
+int row_parts(int N, int V, bool bf16) {
+  const int round = kThreads * (bf16 ? 8 : 4);
+  const int want = (512 + N - 1) / N, most = (V + round - 1) / round;
+  const int p = want < most ? want : most;
+  return p < 1 ? 1 : p > kMaxParts ? kMaxParts : p;
+}
+dim3 grid_of(long long items) { return dim3((unsigned)(items < kMaxGrid ? items : kMaxGrid)); }
+
+template <bool BF16, bool TOP>
+hipError_t logprob_run(const LogprobArgs& a, hipStream_t st) {
+  const int parts = row_parts(a.r.N, a.r.V, BF16);
+  timing_before("logprobs", st);
+  hipLaunchKernelGGL((logprob_kernel<BF16, kThreads, kUnroll, TOP>),
+                     grid_of((long long)a.r.N * parts), dim3(kThreads), 0, st, a, parts);
+  timing_after(st);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (parts == 1) return hipSuccess;
+  timing_before("logprobs_join", st);
+  hipLaunchKernelGGL((logprob_join_kernel<BF16, TOP>), grid_of(a.r.N), dim3(256),
+                     TOP ? sizeof(uint2) * parts * a.top : 0, st, a, parts);
+  timing_after(st);
+  return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t distill_run(const DistillArgs& a, hipStream_t st) {
+  const int parts = row_parts(a.r.N, a.r.V, BF16);
+  const dim3 blk(kThreads);
+  if (a.loss) {
+    timing_before("distill", st);
+    if (a.dz && parts == 1)
+      hipLaunchKernelGGL((distill_kernel<BF16, kThreads, kUnroll, true, true>), grid_of(a.r.N),
+                         blk, 0, st, a, 1);
+    else
+      hipLaunchKernelGGL((distill_kernel<BF16, kThreads, kUnroll, true, false>),
+                         grid_of((long long)a.r.N * parts), blk, 0, st, a, parts);
+    timing_after(st);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (parts == 1) return hipSuccess;
+    timing_before("distill_join", st);
+    hipLaunchKernelGGL((distill_join_kernel<BF16>), grid_of(a.r.N), dim3(256), 0, st, a, parts);
+    timing_after(st);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  if (!a.dz) return hipSuccess;
+  timing_before("distill_grad", st);
+  hipLaunchKernelGGL((distill_kernel<BF16, kThreads, kUnroll, false, true>),
+                     grid_of((long long)a.r.N * parts), blk, 0, st, a, parts);
+  timing_after(st);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t logprob_workspace_bytes(int N, int V, int bf16, int top) {
+  const int parts = row_parts(N, V, bf16 != 0);
+  return parts == 1 ? 0 : (size_t)N * parts * (16 + sizeof(uint2) * top);
+}
+
+hipError_t logprob_launch(const LogprobArgs& a, hipStream_t stream) {
+  if (a.r.bf16)
+    return a.top ? logprob_run<true, true>(a, stream) : logprob_run<true, false>(a, stream);
+  return a.top ? logprob_run<false, true>(a, stream) : logprob_run<false, false>(a, stream);
+}
+
+hipError_t logprob_grad_launch(const LogprobGradArgs& a, hipStream_t stream) {
+  const int parts = row_parts(a.r.N, a.r.V, a.r.bf16 != 0);
+  const dim3 grid = grid_of((long long)a.r.N * parts);
+  timing_before("logprobs_grad", stream);
+  if (a.r.bf16)
+    hipLaunchKernelGGL((logprob_grad_kernel<true, kThreads, kUnroll>), grid, dim3(kThreads), 0,
+                       stream, a, parts);
+  else
+    hipLaunchKernelGGL((logprob_grad_kernel<false, kThreads, kUnroll>), grid, dim3(kThreads), 0,
+                       stream, a, parts);
+  timing_after(stream);
+  return hipGetLastError();
+}
+
+size_t distill_workspace_bytes(int N, int V, int bf16) {
+  const int parts = row_parts(N, V, bf16 != 0);
+  return parts == 1 ? 0 : (size_t)N * parts * 16;
+}
+
+hipError_t distill_launch(const DistillArgs& a, hipStream_t stream) {
+  return a.r.bf16 ? distill_run<true>(a, stream) : distill_run<false>(a, stream);
+}
+
+}  // namespace sru

@@ -30,6 +30,8 @@ _lib = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _S = ctypes.c_size_t
+_L = ctypes.c_longlong
+_F = ctypes.c_float
 
 # name -> (restype, argtypes); mirrors include/sru.h
 _SIGNATURES = {
@@ -58,6 +60,16 @@ _SIGNATURES = {
                              + [_P] * 2 + [_P, _S, _P]),
     "sru_round_bf16": (_I, [_P, _S, _P, _P]),
     "sru_forward_fused_available": (_I, [_I] * 6),
+    "sru_token_logprobs_workspace_bytes": (_S, [_I] * 4),
+    "sru_token_logprobs": (_I, [_P, _L, _I, _P] + [_I] * 3 + [_F] + [_P] * 5 + [_P, _S, _P]),
+    "sru_token_logprobs_backward": (_I, [_P, _L, _I] + [_P] * 7 + [_I] * 3 + [_F, _P, _L, _P]),
+    "sru_distill_workspace_bytes": (_S, [_I] * 3),
+    "sru_distill_forward": (_I, [_P, _L, _I, _P, _P, _I] + [_I] * 3 + [_F] + [_P] * 2
+                            + [_P, _S, _P]),
+    "sru_distill_backward": (_I, [_P, _L, _I, _P, _P, _I, _P, _P] + [_I] * 3
+                             + [_F, _P, _L, _P]),
+    "sru_distill_forward_backward": (_I, [_P, _L, _I, _P, _P, _I, _P] + [_I] * 3
+                                     + [_F, _P, _P, _P, _L] + [_P, _S, _P]),
     "sru_timing_begin": (_I, [_P, _I]),
     "sru_timing_end": (_I, []),
     "sru_timing_label": (ctypes.c_char_p, [_I]),
