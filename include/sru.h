@@ -411,6 +411,45 @@ SRU_API int sru_distill_forward_backward(const void* logits, long long ld, int d
                                          void* dlogits, long long ldd, void* workspace,
                                          size_t workspace_bytes, hipStream_t stream);
 
+/* Residual norm: what lies between two blocks of a residual network, M rows of
+ * width d (1 <= d <= SRU_MAX_NORM_WIDTH), rstd(v) = 1 / sqrt(mean(v^2) + eps):
+ *   n  = y rstd(y) w_post       the block's output, normed
+ *   u  = n gate(z)              SRU_GATE_SILU: z sigma(z); SRU_GATE_SIGMOID
+ *   x_out = x + scale u         the residual sum
+ *   o  = x_out rstd(x_out) w_pre  the next block's input
+ * Rows are contiguous, of the pitch given after each pointer (elements, >= d).
+ * y, z, o and their gradients have type dtype, x, x_out and theirs res_dtype
+ * (dtype, or fp32 beside bf16: a residual stream kept in full precision).
+ * o is computed from x_out before that is rounded.  w_post, scale, w_pre are
+ * fp32 [d]; each may be NULL: no norm of y, scale 1, no o.  z NULL: no gate.
+ * y NULL (with z, w_post, scale, x_out NULL): o is the norm of x.  rstd [M, 2]
+ * receives rstd(y) and rstd(x_out) for the gradient call (0 where not taken).
+ * x_out may be x's own memory.
+ *
+ * The gradient call takes the forward inputs and rstd, and dx_out, do_ (the
+ * gradients of x_out and o; each may be NULL: zeros); it reads no forward
+ * output, so nothing that was rounded enters it.  dx is required; dy, dz,
+ * dw_post, dscale, dw_pre exactly where y, z, w_post, scale, w_pre are given.
+ * dx may be dx_out's own memory. */
+typedef enum { SRU_GATE_SILU = 0, SRU_GATE_SIGMOID = 1 } sru_gate;
+#define SRU_MAX_NORM_WIDTH 16384
+SRU_API int sru_residual_norm_forward(int M, int d, int dtype, int res_dtype, int gate, float eps,
+                                      const void* x, long long ldx, const void* y, long long ldy,
+                                      const void* z, long long ldz, const float* w_post,
+                                      const float* scale, const float* w_pre, void* x_out,
+                                      long long ldx_out, void* o, long long ldo, float* rstd,
+                                      hipStream_t stream);
+SRU_API size_t sru_residual_norm_backward_workspace_bytes(int M, int d);
+SRU_API int sru_residual_norm_backward(int M, int d, int dtype, int res_dtype, int gate,
+                                       const void* x, long long ldx, const void* y, long long ldy,
+                                       const void* z, long long ldz, const float* w_post,
+                                       const float* scale, const float* w_pre, const float* rstd,
+                                       const void* dx_out, long long lddx_out, const void* do_,
+                                       long long lddo, void* dx, long long lddx, void* dy,
+                                       long long lddy, void* dz, long long lddz, float* dw_post,
+                                       float* dscale, float* dw_pre, void* workspace,
+                                       size_t workspace_bytes, hipStream_t stream);
+
 /* ---------------------------------------------------------------------------
  * Measurement hook, per calling thread.  sru_timing_begin arms it with
  * `capacity` events the caller created (hipEventCreate, timing enabled).
@@ -430,7 +469,8 @@ SRU_API int sru_distill_forward_backward(const void* logits, long long ld, int d
  *     fused projection + scan of inference);
  *   vocabulary rows: "logprobs", "distill" (and "logprobs_join",
  *     "distill_join" where a row is cut into parts), "logprobs_grad",
- *     "distill_grad".
+ *     "distill_grad";
+ *   residual norm: "norm", "norm_grad", "norm_sums" (parameter gradients).
  * The caller owns the events and reads them after synchronising.
  * Disarmed (the default), launches record nothing.
  * ------------------------------------------------------------------------- */

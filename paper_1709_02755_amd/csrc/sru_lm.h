@@ -71,4 +71,36 @@ struct DistillArgs {
 size_t distill_workspace_bytes(int N, int V, int bf16);
 hipError_t distill_launch(const DistillArgs& a, hipStream_t stream);
 
+// ------------------------------------------------------------- residual norm
+constexpr int kMaxNormWidth = 16384;  // a row is held in one workgroup's registers
+
+// A matrix of M rows (data may be nullptr: absent), row pitch ld elements.
+struct Rows {
+  const void* p;
+  long long ld;
+};
+struct NormArgs {
+  int M, d;
+  int act_bf16, res_bf16;
+  int silu;  // gate z sigma(z), else sigma(z)
+  float eps;
+  Rows x, y, z;
+  const float* w_post;
+  const float* scale;
+  const float* w_pre;
+  float* rstd;  // [M, 2]: of y and of x_out; out in the forward, in for the gradient
+  // forward
+  Rows x_out, o;
+  // gradient
+  Rows dx_out, go;   // in: gradients of x_out and o
+  Rows dx, dy, dz;   // out
+  float* dw_post;
+  float* dscale;
+  float* dw_pre;
+  float* partial;    // norm_grad_workspace_bytes
+};
+hipError_t norm_launch(const NormArgs& a, hipStream_t stream);
+size_t norm_grad_workspace_bytes(int M, int d);
+hipError_t norm_grad_launch(const NormArgs& a, hipStream_t stream);
+
 }  // namespace sru

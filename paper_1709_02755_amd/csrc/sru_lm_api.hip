@@ -65,8 +65,37 @@ int check_teacher(const int64_t* ids, const void* logits, int dtype, int N, int 
   return aligned(ids, 8) && aligned(logits, elem_size(dtype)) ? SRU_OK : SRU_E_ALIGN;
 }
 
+// One matrix of the residual norm; a missing one is OK unless required.
+struct RowsCheck {
+  int M, d;
+  int operator()(const void* p, long long ld, int dtype, bool required, sru::Rows& r) const {
+    if (!p) {
+      r = sru::Rows{nullptr, 0};
+      return required ? SRU_E_NULLPTR : SRU_OK;
+    }
+    if (ld < d || ld > kMaxElems / M) return SRU_E_SHAPE;
+    if (!aligned(p, elem_size(dtype))) return SRU_E_ALIGN;
+    r = sru::Rows{p, ld};
+    return SRU_OK;
+  }
+};
+
+int check_norm(int M, int d, int dtype, int res_dtype, int gate, sru::NormArgs& a) {
+  if (!valid_dtype(dtype) || (res_dtype != dtype && res_dtype != SRU_DTYPE_FP32))
+    return SRU_E_FLAG;
+  if (gate != SRU_GATE_SILU && gate != SRU_GATE_SIGMOID) return SRU_E_FLAG;
+  if (M <= 0 || d <= 0 || d > SRU_MAX_NORM_WIDTH) return SRU_E_SHAPE;
+  a.M = M;
+  a.d = d;
+  a.act_bf16 = dtype == SRU_DTYPE_BF16;
+  a.res_bf16 = res_dtype == SRU_DTYPE_BF16;
+  a.silu = gate == SRU_GATE_SILU;
+  return SRU_OK;
+}
+
 }  // namespace
 
+static_assert(SRU_MAX_NORM_WIDTH == sru::kMaxNormWidth, "limits");
 static_assert(SRU_MAX_TOP == sru::kMaxTop && SRU_MAX_TEACHER == sru::kMaxTeacher, "limits");
 
 extern "C" {
@@ -203,6 +232,79 @@ int sru_distill_forward_backward(const void* logits, long long ld, int dtype,
   a.ldd = ldd;
   a.workspace = workspace;
   return hip_status(sru::distill_launch(a, stream));
+}
+
+int sru_residual_norm_forward(int M, int d, int dtype, int res_dtype, int gate, float eps,
+                              const void* x, long long ldx, const void* y, long long ldy,
+                              const void* z, long long ldz, const float* w_post,
+                              const float* scale, const float* w_pre, void* x_out,
+                              long long ldx_out, void* o, long long ldo, float* rstd,
+                              hipStream_t stream) {
+  sru::NormArgs a{};
+  if (int e = check_norm(M, d, dtype, res_dtype, gate, a)) return e;
+  if (!std::isfinite(eps) || !(eps > 0.f)) return SRU_E_SHAPE;
+  // without a block's output there is nothing but the norm of x, without
+  // w_pre nothing but the sum
+  if (!y && (z || w_post || scale || x_out || !w_pre)) return SRU_E_NULLPTR;
+  if (!w_pre && o) return SRU_E_NULLPTR;
+  const RowsCheck rows{M, d};
+  if (int e = rows(x, ldx, res_dtype, true, a.x)) return e;
+  if (int e = rows(y, ldy, dtype, false, a.y)) return e;
+  if (int e = rows(z, ldz, dtype, false, a.z)) return e;
+  if (int e = rows(x_out, ldx_out, res_dtype, y != nullptr, a.x_out)) return e;
+  if (int e = rows(o, ldo, dtype, w_pre != nullptr, a.o)) return e;
+  if (!rstd) return SRU_E_NULLPTR;
+  if (!all_aligned({w_post, scale, w_pre, rstd}, 4)) return SRU_E_ALIGN;
+  a.eps = eps;
+  a.w_post = w_post;
+  a.scale = scale;
+  a.w_pre = w_pre;
+  a.rstd = rstd;
+  return hip_status(sru::norm_launch(a, stream));
+}
+
+size_t sru_residual_norm_backward_workspace_bytes(int M, int d) {
+  if (M <= 0 || d <= 0 || d > SRU_MAX_NORM_WIDTH) return 0;
+  return align_up(sru::norm_grad_workspace_bytes(M, d));
+}
+
+int sru_residual_norm_backward(int M, int d, int dtype, int res_dtype, int gate, const void* x,
+                               long long ldx, const void* y, long long ldy, const void* z,
+                               long long ldz, const float* w_post, const float* scale,
+                               const float* w_pre, const float* rstd, const void* dx_out,
+                               long long lddx_out, const void* do_, long long lddo, void* dx,
+                               long long lddx, void* dy, long long lddy, void* dz, long long lddz,
+                               float* dw_post, float* dscale, float* dw_pre, void* workspace,
+                               size_t workspace_bytes, hipStream_t stream) {
+  sru::NormArgs a{};
+  if (int e = check_norm(M, d, dtype, res_dtype, gate, a)) return e;
+  if (!y && (z || w_post || scale || !w_pre)) return SRU_E_NULLPTR;
+  // a gradient for every input that is there, and for no other
+  if (!dy != !y || !dz != !z || !dw_post != !w_post || !dscale != !scale || !dw_pre != !w_pre)
+    return SRU_E_NULLPTR;
+  const RowsCheck rows{M, d};
+  if (int e = rows(x, ldx, res_dtype, true, a.x)) return e;
+  if (int e = rows(y, ldy, dtype, false, a.y)) return e;
+  if (int e = rows(z, ldz, dtype, false, a.z)) return e;
+  if (int e = rows(dx_out, lddx_out, res_dtype, false, a.dx_out)) return e;
+  if (int e = rows(do_, lddo, dtype, false, a.go)) return e;
+  if (int e = rows(dx, lddx, res_dtype, true, a.dx)) return e;
+  if (int e = rows(dy, lddy, dtype, false, a.dy)) return e;
+  if (int e = rows(dz, lddz, dtype, false, a.dz)) return e;
+  if (!rstd) return SRU_E_NULLPTR;
+  if (!all_aligned({w_post, scale, w_pre, rstd, dw_post, dscale, dw_pre}, 4)) return SRU_E_ALIGN;
+  if (int e = check_workspace(sru_residual_norm_backward_workspace_bytes(M, d), workspace,
+                              workspace_bytes))
+    return e;
+  a.w_post = w_post;
+  a.scale = scale;
+  a.w_pre = w_pre;
+  a.rstd = const_cast<float*>(rstd);  // read only by the gradient
+  a.dw_post = dw_post;
+  a.dscale = dscale;
+  a.dw_pre = dw_pre;
+  a.partial = static_cast<float*>(workspace);
+  return hip_status(sru::norm_grad_launch(a, stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,422 @@
+// Between two blocks of a residual network: the norm of the block's output,
+// its gate, the residual scale and sum, and the norm before the next block,
+//   n = y rstd(y) w_post,  u = n gate(z),  x' = x + scale u,  o = x' rstd(x') w_pre
+// with rstd(v) = 1 / sqrt(mean(v^2) + eps), and its gradient.
+//
+// Both are bound by memory: a row's tensors are read once into registers, all
+// in 16-byte loads where the rows allow, its sums are taken there, and the
+// results leave rounded once.  The gradient works x' out again from x, y and z
+// rather than reading x_out, so that no rounded value enters it.
+#include "sru_device.h"
+#include "sru_lm.h"
+
+namespace sru {
+namespace {
+
+template <bool BF16>
+struct Mem {
+  using T = float;
+};
+template <>
+struct Mem<true> {
+  using T = uint16_t;
+};
+
+// VE consecutive elements to and from floats; 16-byte accesses (two for 8
+// fp32 values) unless VE is 1.
+template <bool BF16, int VE>
+__device__ __forceinline__ void load(const typename Mem<BF16>::T* p, float* f) {
+  if constexpr (VE == 1) {
+    if constexpr (BF16) f[0] = __uint_as_float((unsigned)*p << 16);
+    else f[0] = *p;
+  } else if constexpr (BF16) {
+    static_assert(VE == 8, "16 bytes");
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VE; i += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(p + i);
+      f[i] = v.x;
+      f[i + 1] = v.y;
+      f[i + 2] = v.z;
+      f[i + 3] = v.w;
+    }
+  }
+}
+template <bool BF16, int VE>
+__device__ __forceinline__ void store(typename Mem<BF16>::T* p, const float* f) {
+  if constexpr (VE == 1) {
+    if constexpr (BF16) *p = __builtin_bit_cast(uint16_t, (__bf16)f[0]);
+    else *p = f[0];
+  } else if constexpr (BF16) {
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)f[2 * i]) |
+             ((unsigned)__builtin_bit_cast(uint16_t, (__bf16)f[2 * i + 1]) << 16);
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VE; i += 4)
+      *reinterpret_cast<float4*>(p + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+  }
+}
+
+// How a kernel holds a row: NW waves, each thread C chunks of VE consecutive
+// columns, the chunks of a row dealt to its threads in turn.  With one wave to
+// a row a workgroup works on four rows at a time.
+template <int VE_, int C_, int NW_>
+struct Hold {
+  static constexpr int VE = VE_, C = C_, NW = NW_, F = VE_ * C_;
+  static constexpr int ROWS = NW_ == 1 ? 4 : 1;
+  static constexpr int THREADS = 64 * NW_ * ROWS;
+  __device__ static int lane() { return NW == 1 ? threadIdx.x & 63 : threadIdx.x; }
+  __device__ static int sub() { return NW == 1 ? threadIdx.x >> 6 : 0; }
+  __device__ static int col(int c) { return (c * NW * 64 + lane()) * VE; }
+};
+
+// F columns of a row; columns past d are 0.
+template <class H, bool BF16>
+__device__ __forceinline__ void load_row(const void* p, long long off, int d, float (&f)[H::F]) {
+  const auto* q = static_cast<const typename Mem<BF16>::T*>(p) + off;
+#pragma unroll
+  for (int c = 0; c < H::C; ++c) {
+    const int col = H::col(c);
+    if (col < d) {
+      load<BF16, H::VE>(q + col, f + c * H::VE);
+    } else {
+#pragma unroll
+      for (int j = 0; j < H::VE; ++j) f[c * H::VE + j] = 0.f;
+    }
+  }
+}
+template <class H, bool BF16>
+__device__ __forceinline__ void store_row(const void* p, long long off, int d,
+                                          const float (&f)[H::F]) {
+  auto* q = static_cast<typename Mem<BF16>::T*>(const_cast<void*>(p)) + off;
+#pragma unroll
+  for (int c = 0; c < H::C; ++c) {
+    const int col = H::col(c);
+    if (col < d) store<BF16, H::VE>(q + col, f + c * H::VE);
+  }
+}
+
+// The sum over a row's threads, in each of them, always in the same order.
+template <class H>
+__device__ __forceinline__ float row_sum(float v, float* lds) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+  if constexpr (H::NW > 1) {
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < H::NW; ++w) v += lds[w];
+    __syncthreads();
+  }
+  return v;
+}
+
+__device__ __forceinline__ float rstd_of(float sum, int d, float eps) {
+  return 1.f / sqrtf(sum / (float)d + eps);
+}
+
+template <class H, bool ABF, bool RBF>
+__global__ __launch_bounds__(H::THREADS) void norm_kernel(NormArgs a) {
+  __shared__ float lds[H::NW];
+  const int d = a.d;
+  for (long long m0 = (long long)blockIdx.x * H::ROWS; m0 < a.M;
+       m0 += (long long)gridDim.x * H::ROWS) {
+    const long long m = m0 + H::sub();
+    if (H::NW == 1 && m >= a.M) break;  // a wave's own row: it meets no barrier
+    float x[H::F], rx = 0.f, ry = 0.f;
+    load_row<H, RBF>(a.x.p, m * a.x.ld, d, x);
+    if (a.y.p) {
+      float y[H::F], z[H::F], w[H::F];
+      load_row<H, ABF>(a.y.p, m * a.y.ld, d, y);
+      if (a.z.p) load_row<H, ABF>(a.z.p, m * a.z.ld, d, z);
+      if (a.w_post) {
+        load_row<H, false>(a.w_post, 0, d, w);
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < H::F; ++j) s = fmaf(y[j], y[j], s);
+        ry = rstd_of(row_sum<H>(s, lds), d, a.eps);
+#pragma unroll
+        for (int j = 0; j < H::F; ++j) y[j] = y[j] * ry * w[j];
+      }
+      if (a.z.p) {
+#pragma unroll
+        for (int j = 0; j < H::F; ++j) {
+          const float sg = sigmoid_fast(z[j]);
+          y[j] *= a.silu ? z[j] * sg : sg;
+        }
+      }
+      if (a.scale) load_row<H, false>(a.scale, 0, d, w);
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) x[j] = a.scale ? fmaf(w[j], y[j], x[j]) : x[j] + y[j];
+      store_row<H, RBF>(a.x_out.p, m * a.x_out.ld, d, x);
+    }
+    if (a.w_pre) {
+      float w[H::F];
+      load_row<H, false>(a.w_pre, 0, d, w);
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) s = fmaf(x[j], x[j], s);
+      rx = rstd_of(row_sum<H>(s, lds), d, a.eps);
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) w[j] *= x[j] * rx;
+      store_row<H, ABF>(a.o.p, m * a.o.ld, d, w);
+    }
+    if (H::lane() == 0) {
+      a.rstd[2 * m] = ry;
+      a.rstd[2 * m + 1] = rx;
+    }
+  }
+}
+
+// t = do w_pre, xh = x' rstd_x:  dx = dx_out + rstd_x (t - xh mean(t xh));
+// du = dx scale, dz = du n gate'(z), dn = du gate(z);
+// t = dn w_post, yh = y rstd_y:  dy = rstd_y (t - yh mean(t yh)).
+// Every workgroup adds its rows' terms of the three parameter gradients in
+// registers and leaves one row of sums, [workgroup, 3, d].
+template <class H, bool ABF, bool RBF>
+__global__ __launch_bounds__(H::THREADS) void norm_grad_kernel(NormArgs a) {
+  __shared__ float lds[H::NW];
+  __shared__ float sums[H::ROWS > 1 ? H::ROWS * 64 * H::F : 1];
+  const int d = a.d;
+  float gw_post[H::F], gscale[H::F], gw_pre[H::F];
+#pragma unroll
+  for (int j = 0; j < H::F; ++j) gw_post[j] = gscale[j] = gw_pre[j] = 0.f;
+
+  for (long long m0 = (long long)blockIdx.x * H::ROWS; m0 < a.M;
+       m0 += (long long)gridDim.x * H::ROWS) {
+    const long long m = m0 + H::sub();
+    if (H::NW == 1 && m >= a.M) break;
+    float x[H::F], y[H::F], z[H::F], u[H::F], dx[H::F], w[H::F];
+    load_row<H, RBF>(a.x.p, m * a.x.ld, d, x);
+    if (a.y.p) load_row<H, ABF>(a.y.p, m * a.y.ld, d, y);
+    if (a.z.p) load_row<H, ABF>(a.z.p, m * a.z.ld, d, z);
+    if (a.dx_out.p) {
+      load_row<H, RBF>(a.dx_out.p, m * a.dx_out.ld, d, dx);
+    } else {
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) dx[j] = 0.f;
+    }
+    const float ry = a.w_post ? a.rstd[2 * m] : 1.f;
+    // y becomes yh; u = n gate(z)
+    if (a.y.p) {
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) u[j] = y[j] *= ry;
+      if (a.w_post) {
+        load_row<H, false>(a.w_post, 0, d, w);
+#pragma unroll
+        for (int j = 0; j < H::F; ++j) u[j] *= w[j];
+      }
+      if (a.z.p) {
+#pragma unroll
+        for (int j = 0; j < H::F; ++j) {
+          const float sg = sigmoid_fast(z[j]);
+          u[j] *= a.silu ? z[j] * sg : sg;
+        }
+      }
+      if (a.scale) load_row<H, false>(a.scale, 0, d, w);
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) x[j] = a.scale ? fmaf(w[j], u[j], x[j]) : x[j] + u[j];
+    }
+    if (a.w_pre && a.go.p) {
+      const float rx = a.rstd[2 * m + 1];
+      float t[H::F];
+      load_row<H, ABF>(a.go.p, m * a.go.ld, d, t);
+      load_row<H, false>(a.w_pre, 0, d, w);
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) {
+        x[j] *= rx;
+        gw_pre[j] = fmaf(t[j], x[j], gw_pre[j]);
+        t[j] *= w[j];
+        s = fmaf(t[j], x[j], s);
+      }
+      s = row_sum<H>(s, lds) / (float)d;
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) dx[j] += rx * (t[j] - x[j] * s);
+    }
+    store_row<H, RBF>(a.dx.p, m * a.dx.ld, d, dx);
+    if (!a.y.p) continue;
+#pragma unroll
+    for (int j = 0; j < H::F; ++j) gscale[j] = fmaf(dx[j], u[j], gscale[j]);
+    // dx becomes du
+    if (a.scale) {
+      load_row<H, false>(a.scale, 0, d, w);
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) dx[j] *= w[j];
+    }
+    if (a.w_post) {
+      load_row<H, false>(a.w_post, 0, d, w);
+    } else {
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) w[j] = 1.f;
+    }
+    // z becomes dz, dx becomes dn
+    if (a.z.p) {
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) {
+        const float sg = sigmoid_fast(z[j]);
+        const float gate = a.silu ? z[j] * sg : sg;
+        const float slope = a.silu ? fmaf(gate, 1.f - sg, sg) : sg * (1.f - sg);
+        z[j] = dx[j] * (y[j] * w[j]) * slope;
+        dx[j] *= gate;
+      }
+      store_row<H, ABF>(a.dz.p, m * a.dz.ld, d, z);
+    }
+    if (a.w_post) {
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) {
+        gw_post[j] = fmaf(dx[j], y[j], gw_post[j]);
+        dx[j] *= w[j];
+        s = fmaf(dx[j], y[j], s);
+      }
+      s = row_sum<H>(s, lds) / (float)d;
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) dx[j] = ry * (dx[j] - y[j] * s);
+    }
+    store_row<H, ABF>(a.dy.p, m * a.dy.ld, d, dx);
+  }
+
+  // the workgroup's sums, its rows' waves added in order
+  float* const out = a.partial + (long long)blockIdx.x * 3 * d;
+  auto leave = [&](float(&g)[H::F], int q) {
+    if constexpr (H::ROWS > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) sums[(H::sub() * H::F + j) * 64 + H::lane()] = g[j];
+      __syncthreads();
+      if (H::sub() != 0) return;
+#pragma unroll
+      for (int j = 0; j < H::F; ++j) {
+        float s = g[j];
+#pragma unroll
+        for (int r = 1; r < H::ROWS; ++r) s += sums[(r * H::F + j) * 64 + H::lane()];
+        g[j] = s;
+      }
+    }
+    store_row<H, false>(out, (long long)q * d, d, g);
+  };
+  if (a.dw_post) leave(gw_post, 0);
+  if (a.dscale) leave(gscale, 1);
+  if (a.dw_pre) leave(gw_pre, 2);
+}
+
+// Column sums of [rows, 3, d]: 64 columns a workgroup, its 16 waves take every
+// 16th row and meet in a fixed order.
+__global__ __launch_bounds__(1024) void norm_sums_kernel(NormArgs a, int rows) {
+  __shared__ float red[16 * 64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int groups = (a.d + 63) / 64;
+  const int q = blockIdx.x / groups, col = (blockIdx.x - q * groups) * 64 + lane;
+  float* const out = q == 0 ? a.dw_post : q == 1 ? a.dscale : a.dw_pre;
+  if (!out) return;  // the whole workgroup
+  float s = 0.f;
+  if (col < a.d) {
+    const float* p = a.partial + (long long)q * a.d + col;
+    const long long stride = 3LL * a.d;
+#pragma unroll 8
+    for (int r = w; r < rows; r += 16) s += p[r * stride];
+  }
+  red[w * 64 + lane] = s;
+  __syncthreads();
+  if (w == 0 && col < a.d) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += red[i * 64 + lane];
+    out[col] = s;
+  }
+}
+
+// Workgroups of the gradient: each leaves one row of sums, so only about as
+// many as run at a time.
+int grad_blocks(int M, int d) {
+  const int rows = d <= 1024 ? 4 : 1;  // rows a workgroup has at a time
+  const int most = d <= 1024 ? 512 : d <= 2048 ? 512 : d <= 4096 ? 512 : 256;
+  const int want = (M + rows - 1) / rows;
+  return want < most ? want : most;
+}
+
+template <class H, bool ABF, bool RBF>
+hipError_t launch(const NormArgs& a, bool grad, hipStream_t st) {
+  if (grad) {
+    const int blocks = grad_blocks(a.M, a.d);
+    timing_before("norm_grad", st);
+    hipLaunchKernelGGL((norm_grad_kernel<H, ABF, RBF>), dim3(blocks), dim3(H::THREADS), 0, st, a);
+    timing_after(st);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (!a.dw_post && !a.dscale && !a.dw_pre) return hipSuccess;
+    timing_before("norm_sums", st);
+    hipLaunchKernelGGL(norm_sums_kernel, dim3(3 * ((a.d + 63) / 64)), dim3(1024), 0, st, a,
+                       blocks);
+    timing_after(st);
+    return hipGetLastError();
+  }
+  const long long want = ((long long)a.M + H::ROWS - 1) / H::ROWS;
+  timing_before("norm", st);
+  hipLaunchKernelGGL((norm_kernel<H, ABF, RBF>),
+                     dim3((unsigned)(want < kMaxGrid ? want : kMaxGrid)), dim3(H::THREADS), 0, st,
+                     a);
+  timing_after(st);
+  return hipGetLastError();
+}
+
+// Waves and columns a thread by the width: a row's columns stay in registers,
+// 8 to a thread (16 up to 1024 columns, where one wave then holds a row and
+// needs no barrier, and past 8192).
+template <int VE, bool ABF, bool RBF>
+hipError_t by_width(const NormArgs& a, bool grad, hipStream_t st) {
+  if (a.d <= 512) return launch<Hold<VE, 8 / VE, 1>, ABF, RBF>(a, grad, st);
+  if (a.d <= 1024) return launch<Hold<VE, 16 / VE, 1>, ABF, RBF>(a, grad, st);
+  if (a.d <= 2048) return launch<Hold<VE, 8 / VE, 4>, ABF, RBF>(a, grad, st);
+  if (a.d <= 4096) return launch<Hold<VE, 8 / VE, 8>, ABF, RBF>(a, grad, st);
+  if (a.d <= 8192) return launch<Hold<VE, 8 / VE, 16>, ABF, RBF>(a, grad, st);
+  return launch<Hold<VE, 16 / VE, 16>, ABF, RBF>(a, grad, st);
+}
+
+// 16-byte accesses need every row of every tensor to start on 16 bytes.
+bool vector_ok(const NormArgs& a) {
+  const int ve = a.act_bf16 ? 8 : 4;
+  if (a.d % ve) return false;
+  auto rows = [](const Rows& r, bool bf16) {
+    return !r.p || ((reinterpret_cast<uintptr_t>(r.p) | (uintptr_t)(r.ld * (bf16 ? 2 : 4))) & 15) == 0;
+  };
+  auto vec = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+  const bool A = a.act_bf16, R = a.res_bf16;
+  return rows(a.x, R) && rows(a.y, A) && rows(a.z, A) && rows(a.x_out, R) && rows(a.o, A) &&
+         rows(a.dx_out, R) && rows(a.go, A) && rows(a.dx, R) && rows(a.dy, A) && rows(a.dz, A) &&
+         vec(a.w_post) && vec(a.scale) && vec(a.w_pre);
+}
+
+hipError_t dispatch(const NormArgs& a, bool grad, hipStream_t st) {
+  const bool v = vector_ok(a);
+  if (!a.act_bf16)
+    return v ? by_width<4, false, false>(a, grad, st) : by_width<1, false, false>(a, grad, st);
+  if (!a.res_bf16)
+    return v ? by_width<8, true, false>(a, grad, st) : by_width<1, true, false>(a, grad, st);
+  return v ? by_width<8, true, true>(a, grad, st) : by_width<1, true, true>(a, grad, st);
+}
+
+}  // namespace
+
+hipError_t norm_launch(const NormArgs& a, hipStream_t stream) { return dispatch(a, false, stream); }
+
+size_t norm_grad_workspace_bytes(int M, int d) {
+  return sizeof(float) * 3 * (size_t)d * grad_blocks(M, d);
+}
+
+hipError_t norm_grad_launch(const NormArgs& a, hipStream_t stream) {
+  return dispatch(a, true, stream);
+}
+
+}  // namespace sru

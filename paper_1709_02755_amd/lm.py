@@ -1,6 +1,6 @@
 """Operators of a language model around the SRU layer (argument marshalling
-over libsru.so, as in ``sru``): log probabilities of tokens and distillation at
-its head.
+over libsru.so, as in ``sru``): norms, gate and residual scale between its
+blocks, log probabilities of tokens and distillation at its head.
 
 Activations and logits are float32 or bfloat16; parameters, states, statistics
 and losses are float32.  Every call checks its tensors, runs on the current
@@ -17,6 +17,7 @@ from .sru import _check, _ptr, _req, _ws
 
 DTYPE_FP32, DTYPE_BF16 = 0, 1
 MAX_TOP, MAX_TEACHER = 64, 1024
+GATE_SILU, GATE_SIGMOID = 0, 1
 
 _CODES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
 
@@ -213,3 +214,122 @@ def distill_forward_backward(logits, teacher_ids, teacher_logits, dloss, tempera
                                           sru._stream())
     _check(st, "sru_distill_forward_backward")
     return o
+
+
+def _row_pitch(t, name, shape, dtype, device):
+    """The distance of consecutive rows of a [..., d] tensor (None: 0)."""
+    if t is None:
+        return 0
+    if t.__class__ is torch.Tensor and sru._fits(t, shape, dtype, device):
+        return shape[-1]
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if not sru._on_gpu(t):
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    # leading dimensions of more than one row, from the last: one pitch for all
+    ld, span = None, 1
+    for n, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n > 1:
+            if ld is None:
+                ld = step
+            elif step != ld * span:
+                raise ValueError(f"{name} must have rows at equal distances")
+            span *= n
+    d = shape[-1]
+    if (d > 1 and t.stride(-1) != 1) or (ld is not None and ld < d):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return d if ld is None else ld
+
+
+def _norm_inputs(x, y, z, w_post, scale, w_pre):
+    """Checked inputs: M, d, activation type, its code, residual code, device,
+    and the pitches of x, y and z."""
+    res = _dtype(x, "x")
+    if x.dim() < 1:
+        raise ValueError("x must have a last dimension")
+    dv = _here(x, "x")
+    shape = x.shape
+    d = shape[-1]
+    if y is None:
+        if w_pre is None or w_post is not None or z is not None or scale is not None:
+            raise ValueError("without y there is only the norm of x: give w_pre alone")
+        act, code = x.dtype, res
+    else:
+        act, code = y.dtype if isinstance(y, torch.Tensor) else None, _dtype(y, "y")
+        if x.dtype != act and x.dtype != _F32:
+            raise ValueError(f"x must be {act} or float32, got {x.dtype}")
+    pitch = (_row_pitch(x, "x", shape, x.dtype, dv), _row_pitch(y, "y", shape, act, dv),
+             _row_pitch(z, "z", shape, act, dv))
+    for n, w in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
+        _req(w, n, (d,), optional=True, device=dv)
+    return x.numel() // d if d else 0, d, act, code, res, dv, pitch
+
+
+def _row_out(out, name, shape, dtype, device):
+    """(out[name] or a new tensor, its row pitch)."""
+    t = None if out is None else out.get(name)
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device), shape[-1]
+    return t, _row_pitch(t, name, shape, dtype, device)
+
+
+def residual_norm_forward(x, y=None, w_post=None, z=None, scale=None, w_pre=None,
+                          gate=GATE_SILU, eps=1e-6, out=None):
+    """Between two blocks: dict(x_out, o, rstd) with
+
+        x_out = x + scale * (y rstd(y) w_post) * gate(z)
+        o     = x_out rstd(x_out) w_pre,      rstd(v) = 1 / sqrt(mean(v^2) + eps)
+
+    over the last dimension.  x is the residual stream [..., d], y the block's
+    output, z the gate's input (z sigma(z), or sigma(z) with GATE_SIGMOID);
+    w_post, scale and w_pre are float32 [d].  Each of w_post, z, scale and w_pre
+    may be None (no norm of y, no gate, scale 1, no o); without y, o is the norm
+    of x.  x may be float32 beside bfloat16 activations.  Rows may be strided
+    (slices of a projection).  out may hold x_out (x itself), o and rstd."""
+    M, d, act, code, res, dv, (ldx, ldy, ldz) = _norm_inputs(x, y, z, w_post, scale, w_pre)
+    x_out, o, ldxo, ldo = None, None, 0, 0
+    if y is not None:
+        x_out, ldxo = _row_out(out, "x_out", x.shape, x.dtype, dv)
+    if w_pre is not None:
+        o, ldo = _row_out(out, "o", x.shape, act, dv)
+    rstd = _out(out, "rstd", tuple(x.shape[:-1]) + (2,), _F32, dv)
+    st = sru.lib().sru_residual_norm_forward(M, d, code, res, gate, eps, _ptr(x), ldx, _ptr(y),
+                                             ldy, _ptr(z), ldz, _ptr(w_post), _ptr(scale),
+                                             _ptr(w_pre), _ptr(x_out), ldxo, _ptr(o), ldo,
+                                             _ptr(rstd), sru._stream())
+    _check(st, "sru_residual_norm_forward")
+    return dict(x_out=x_out, o=o, rstd=rstd)
+
+
+def residual_norm_backward(x, y, rstd, dx_out=None, do=None, w_post=None, z=None, scale=None,
+                           w_pre=None, gate=GATE_SILU, eps=1e-6, out=None, ws=None):
+    """Gradients of residual_norm_forward, given its inputs, its rstd (which
+    holds eps) and the gradients of x_out and o (None: zeros): dict(dx, dy, dz,
+    dw_post, dscale, dw_pre), None where the input was.  out may hold any of
+    them (dx may be dx_out itself, dy and dz slices of a larger tensor)."""
+    M, d, act, code, res, dv, (ldx, ldy, ldz) = _norm_inputs(x, y, z, w_post, scale, w_pre)
+    shape = x.shape
+    _req(rstd, "rstd", tuple(shape[:-1]) + (2,), device=dv)
+    lddxo = _row_pitch(dx_out, "dx_out", shape, x.dtype, dv)
+    lddo = _row_pitch(do, "do", shape, act, dv)
+    g = {}
+    g["dx"], lddx = _row_out(out, "dx", shape, x.dtype, dv)
+    g["dy"], lddy = _row_out(out, "dy", shape, act, dv) if y is not None else (None, 0)
+    g["dz"], lddz = _row_out(out, "dz", shape, act, dv) if z is not None else (None, 0)
+    for n, w in (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre)):
+        g[n] = None if w is None else _out(out, n, (d,), _F32, dv)
+    lib = sru.lib()
+    ws, nbytes = _ws(ws, lib.sru_residual_norm_backward_workspace_bytes(M, d), dv)
+    st = lib.sru_residual_norm_backward(
+        M, d, code, res, gate, _ptr(x), ldx, _ptr(y), ldy, _ptr(z), ldz, _ptr(w_post),
+        _ptr(scale), _ptr(w_pre), _ptr(rstd), _ptr(dx_out), lddxo, _ptr(do), lddo, _ptr(g["dx"]),
+        lddx, _ptr(g["dy"]), lddy, _ptr(g["dz"]), lddz, _ptr(g["dw_post"]), _ptr(g["dscale"]),
+        _ptr(g["dw_pre"]), _ptr(ws), nbytes, sru._stream())
+    _check(st, "sru_residual_norm_backward")
+    return g

@@ -70,6 +70,11 @@ _SIGNATURES = {
                              + [_F, _P, _L, _P]),
     "sru_distill_forward_backward": (_I, [_P, _L, _I, _P, _P, _I, _P] + [_I] * 3
                                      + [_F, _P, _P, _P, _L] + [_P, _S, _P]),
+    "sru_residual_norm_forward": (_I, [_I] * 5 + [_F] + [_P, _L] * 3 + [_P] * 3 + [_P, _L] * 2
+                                  + [_P, _P]),
+    "sru_residual_norm_backward_workspace_bytes": (_S, [_I] * 2),
+    "sru_residual_norm_backward": (_I, [_I] * 5 + [_P, _L] * 3 + [_P] * 4 + [_P, _L] * 5
+                                   + [_P] * 3 + [_P, _S, _P]),
     "sru_timing_begin": (_I, [_P, _I]),
     "sru_timing_end": (_I, []),
     "sru_timing_label": (ctypes.c_char_p, [_I]),
