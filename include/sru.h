@@ -450,6 +450,49 @@ SRU_API int sru_residual_norm_backward(int M, int d, int dtype, int res_dtype, i
                                        float* dscale, float* dw_pre, void* workspace,
                                        size_t workspace_bytes, hipStream_t stream);
 
+/* Gated linear recurrence over L steps of B sequences, every feature j by itself:
+ *   s = sigma(r_t), g = sigma(i_t), a_t = exp(-c softplus(lam_j) s)
+ *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) g x_t
+ * x, r, i, H and the gradients dH, dx, dr, di are [L, B, d] of one type, features
+ * contiguous, with the distance of consecutive steps (_t) and of sequences (_b)
+ * in elements after each pointer (>= 0; inputs may repeat, outputs must not
+ * overlap; so either order of L and B, and slices of one projection, will do).
+ * lam [d]; c >= 0 (finite); h0, h_last, dh0, dh_last [B, d] (NULL: zeros in, not
+ * wanted out; h_last may be h0's own memory).
+ *   pad_mask [L, B] as above: a padded step leaves the state, outputs 0, and
+ *     nothing of it (whatever it holds) enters a result or a gradient
+ *   reset [L, B] uint8 or NULL, nonzero: a new document starts here, a_t = 0 and
+ *     h_t = g x_t; what came before does not reach it, not even as NaN
+ *   states [ceil(L / SRU_LRU_STEPS), B, d]: the state before every
+ *     SRU_LRU_STEPS-th step, which the gradient call reads (it reads no H);
+ *     NULL in the forward: inference
+ * One step with h0 = h_last is the form for single tokens; it needs no
+ * workspace, nor does any L <= SRU_LRU_SEGMENT in the forward.  Longer
+ * sequences are cut into segments, each one workgroup's, whose maps meet in
+ * the workspace; the results do not depend on the order in which they ran.
+ * A sequence cut into consecutive calls (h_last -> h0) agrees with one call to
+ * fp32 rounding. */
+#define SRU_LRU_STEPS 8
+#define SRU_LRU_SEGMENT 128
+SRU_API size_t sru_lru_forward_workspace_bytes(int L, int B, int d);
+SRU_API int sru_lru_forward(int L, int B, int d, int dtype, const void* x, long long x_t,
+                            long long x_b, const void* r, long long r_t, long long r_b,
+                            const void* i, long long i_t, long long i_b, const float* lam,
+                            float c, const float* h0, const uint8_t* pad_mask,
+                            const uint8_t* reset, void* H, long long H_t, long long H_b,
+                            float* h_last, float* states, void* workspace,
+                            size_t workspace_bytes, hipStream_t stream);
+SRU_API size_t sru_lru_backward_workspace_bytes(int L, int B, int d);
+SRU_API int sru_lru_backward(int L, int B, int d, int dtype, const void* x, long long x_t,
+                             long long x_b, const void* r, long long r_t, long long r_b,
+                             const void* i, long long i_t, long long i_b, const float* lam,
+                             float c, const float* states, const void* dH, long long dH_t,
+                             long long dH_b, const float* dh_last, const uint8_t* pad_mask,
+                             const uint8_t* reset, void* dx, long long dx_t, long long dx_b,
+                             void* dr, long long dr_t, long long dr_b, void* di, long long di_t,
+                             long long di_b, float* dlam, float* dh0, void* workspace,
+                             size_t workspace_bytes, hipStream_t stream);
+
 /* ---------------------------------------------------------------------------
  * Measurement hook, per calling thread.  sru_timing_begin arms it with
  * `capacity` events the caller created (hipEventCreate, timing enabled).
@@ -470,7 +513,9 @@ SRU_API int sru_residual_norm_backward(int M, int d, int dtype, int res_dtype, i
  *   vocabulary rows: "logprobs", "distill" (and "logprobs_join",
  *     "distill_join" where a row is cut into parts), "logprobs_grad",
  *     "distill_grad";
- *   residual norm: "norm", "norm_grad", "norm_sums" (parameter gradients).
+ *   residual norm: "norm", "norm_grad", "norm_sums" (parameter gradients);
+ *   gated linear recurrence: "lru", "lru_grad", "lru_sums" (gradient of lam),
+ *     "lru_clear" (the segments' words, with several segments).
  * The caller owns the events and reads them after synchronising.
  * Disarmed (the default), launches record nothing.
  * ------------------------------------------------------------------------- */

@@ -103,4 +103,40 @@ hipError_t norm_launch(const NormArgs& a, hipStream_t stream);
 size_t norm_grad_workspace_bytes(int M, int d);
 hipError_t norm_grad_launch(const NormArgs& a, hipStream_t stream);
 
+// ------------------------------------------------- gated linear recurrence
+constexpr int kLruSteps = 8;  // steps a wave holds; a state is kept for each
+
+// [L, B, d] with contiguous features; distances of steps and of sequences in
+// elements.
+struct Seq {
+  const void* p;
+  long long st, sb;
+};
+struct LruArgs {
+  int L, B, d, bf16;
+  Seq x, r, i;
+  const float* lam;
+  float c;
+  const uint8_t* mask;   // [L, B] or nullptr
+  const uint8_t* reset;  // [L, B] or nullptr
+  // forward
+  const float* h0;
+  Seq h;
+  float* h_last;
+  float* states;  // [ceil(L / kLruSteps), B, d]; out, or in for the gradient
+  // gradient
+  Seq dh;
+  const float* dh_last;
+  Seq dx, dr, di;
+  float* dlam;
+  float* dh0;
+  void* workspace;
+};
+size_t lru_workspace_bytes(int L, int B, int d);
+size_t lru_grad_workspace_bytes(int L, int B, int d);
+// Workgroups of a call (they must fit a launch).
+long long lru_blocks(int L, int B, int d);
+hipError_t lru_launch(const LruArgs& a, hipStream_t stream);
+hipError_t lru_grad_launch(const LruArgs& a, hipStream_t stream);
+
 }  // namespace sru

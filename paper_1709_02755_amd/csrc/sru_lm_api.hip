@@ -93,8 +93,37 @@ int check_norm(int M, int d, int dtype, int res_dtype, int gate, sru::NormArgs& 
   return SRU_OK;
 }
 
+// One [L, B, d] tensor of the recurrence.
+struct SeqCheck {
+  int L, B, d, dtype;
+  int operator()(const void* p, long long st, long long sb, bool out, sru::Seq& s) const {
+    if (!p) return SRU_E_NULLPTR;
+    if (st < 0 || sb < 0 || st > kMaxElems / L || sb > kMaxElems / B) return SRU_E_SHAPE;
+    // an output's steps and sequences lie apart
+    if (out && L > 1 && st < d) return SRU_E_SHAPE;
+    if (out && B > 1 && sb < d) return SRU_E_SHAPE;
+    if (out && L > 1 && B > 1 && st < sb * (B - 1) + d && sb < st * (L - 1) + d)
+      return SRU_E_SHAPE;
+    if (!aligned(p, elem_size(dtype))) return SRU_E_ALIGN;
+    // the distance over a dimension of one does not count
+    s = sru::Seq{p, L > 1 ? st : 0, B > 1 ? sb : 0};
+    return SRU_OK;
+  }
+};
+
+int check_lru(int L, int B, int d, int dtype, float c) {
+  if (!valid_dtype(dtype)) return SRU_E_FLAG;
+  if (L <= 0 || B <= 0 || d <= 0) return SRU_E_SHAPE;
+  if ((long long)B * d > INT_MAX || (long long)L * B > INT_MAX) return SRU_E_SHAPE;
+  // 1024 threads a workgroup, below 2^32 in a launch
+  if (sru::lru_blocks(L, B, d) >= 1LL << 22) return SRU_E_SHAPE;
+  if (!std::isfinite(c) || c < 0.f) return SRU_E_SHAPE;
+  return SRU_OK;
+}
+
 }  // namespace
 
+static_assert(SRU_LRU_STEPS == sru::kLruSteps, "steps");
 static_assert(SRU_MAX_NORM_WIDTH == sru::kMaxNormWidth, "limits");
 static_assert(SRU_MAX_TOP == sru::kMaxTop && SRU_MAX_TEACHER == sru::kMaxTeacher, "limits");
 
@@ -305,6 +334,88 @@ int sru_residual_norm_backward(int M, int d, int dtype, int res_dtype, int gate,
   a.dw_pre = dw_pre;
   a.partial = static_cast<float*>(workspace);
   return hip_status(sru::norm_grad_launch(a, stream));
+}
+
+size_t sru_lru_forward_workspace_bytes(int L, int B, int d) {
+  if (check_lru(L, B, d, SRU_DTYPE_FP32, 0.f) != SRU_OK) return 0;
+  return align_up(sru::lru_workspace_bytes(L, B, d));
+}
+
+int sru_lru_forward(int L, int B, int d, int dtype, const void* x, long long x_t, long long x_b,
+                    const void* r, long long r_t, long long r_b, const void* i, long long i_t,
+                    long long i_b, const float* lam, float c, const float* h0,
+                    const uint8_t* pad_mask, const uint8_t* reset, void* H, long long H_t,
+                    long long H_b, float* h_last, float* states, void* workspace,
+                    size_t workspace_bytes, hipStream_t stream) {
+  if (int e = check_lru(L, B, d, dtype, c)) return e;
+  sru::LruArgs a{};
+  const SeqCheck seq{L, B, d, dtype};
+  if (int e = seq(x, x_t, x_b, false, a.x)) return e;
+  if (int e = seq(r, r_t, r_b, false, a.r)) return e;
+  if (int e = seq(i, i_t, i_b, false, a.i)) return e;
+  if (int e = seq(H, H_t, H_b, true, a.h)) return e;
+  if (!lam) return SRU_E_NULLPTR;
+  if (!all_aligned({lam, h0, h_last, states}, 4)) return SRU_E_ALIGN;
+  if (int e = check_workspace(sru_lru_forward_workspace_bytes(L, B, d), workspace,
+                              workspace_bytes))
+    return e;
+  a.L = L;
+  a.B = B;
+  a.d = d;
+  a.bf16 = dtype == SRU_DTYPE_BF16;
+  a.lam = lam;
+  a.c = c;
+  a.mask = pad_mask;
+  a.reset = reset;
+  a.h0 = h0;
+  a.h_last = h_last;
+  a.states = states;
+  a.workspace = workspace;
+  return hip_status(sru::lru_launch(a, stream));
+}
+
+size_t sru_lru_backward_workspace_bytes(int L, int B, int d) {
+  if (check_lru(L, B, d, SRU_DTYPE_FP32, 0.f) != SRU_OK) return 0;
+  return align_up(sru::lru_grad_workspace_bytes(L, B, d));
+}
+
+int sru_lru_backward(int L, int B, int d, int dtype, const void* x, long long x_t, long long x_b,
+                     const void* r, long long r_t, long long r_b, const void* i, long long i_t,
+                     long long i_b, const float* lam, float c, const float* states,
+                     const void* dH, long long dH_t, long long dH_b, const float* dh_last,
+                     const uint8_t* pad_mask, const uint8_t* reset, void* dx, long long dx_t,
+                     long long dx_b, void* dr, long long dr_t, long long dr_b, void* di,
+                     long long di_t, long long di_b, float* dlam, float* dh0, void* workspace,
+                     size_t workspace_bytes, hipStream_t stream) {
+  if (int e = check_lru(L, B, d, dtype, c)) return e;
+  sru::LruArgs a{};
+  const SeqCheck seq{L, B, d, dtype};
+  if (int e = seq(x, x_t, x_b, false, a.x)) return e;
+  if (int e = seq(r, r_t, r_b, false, a.r)) return e;
+  if (int e = seq(i, i_t, i_b, false, a.i)) return e;
+  if (int e = seq(dH, dH_t, dH_b, false, a.dh)) return e;
+  if (int e = seq(dx, dx_t, dx_b, true, a.dx)) return e;
+  if (int e = seq(dr, dr_t, dr_b, true, a.dr)) return e;
+  if (int e = seq(di, di_t, di_b, true, a.di)) return e;
+  if (any_null({lam, states, dlam})) return SRU_E_NULLPTR;
+  if (!all_aligned({lam, states, dh_last, dlam, dh0}, 4)) return SRU_E_ALIGN;
+  if (int e = check_workspace(sru_lru_backward_workspace_bytes(L, B, d), workspace,
+                              workspace_bytes))
+    return e;
+  a.L = L;
+  a.B = B;
+  a.d = d;
+  a.bf16 = dtype == SRU_DTYPE_BF16;
+  a.lam = lam;
+  a.c = c;
+  a.mask = pad_mask;
+  a.reset = reset;
+  a.states = const_cast<float*>(states);  // read only by the gradient
+  a.dh_last = dh_last;
+  a.dlam = dlam;
+  a.dh0 = dh0;
+  a.workspace = workspace;
+  return hip_status(sru::lru_grad_launch(a, stream));
 }
 
 }  // extern "C"

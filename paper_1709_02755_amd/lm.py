@@ -1,6 +1,7 @@
 """Operators of a language model around the SRU layer (argument marshalling
-over libsru.so, as in ``sru``): norms, gate and residual scale between its
-blocks, log probabilities of tokens and distillation at its head.
+over libsru.so, as in ``sru``): a gated linear recurrence, norms, gate and
+residual scale between blocks, log probabilities of tokens and distillation at
+the head.
 
 Activations and logits are float32 or bfloat16; parameters, states, statistics
 and losses are float32.  Every call checks its tensors, runs on the current
@@ -18,6 +19,7 @@ from .sru import _check, _ptr, _req, _ws
 DTYPE_FP32, DTYPE_BF16 = 0, 1
 MAX_TOP, MAX_TEACHER = 64, 1024
 GATE_SILU, GATE_SIGMOID = 0, 1
+LRU_STEPS, LRU_SEGMENT = 8, 128
 
 _CODES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
 
@@ -333,3 +335,114 @@ def residual_norm_backward(x, y, rstd, dx_out=None, do=None, w_post=None, z=None
         _ptr(g["dw_pre"]), _ptr(ws), nbytes, sru._stream())
     _check(st, "sru_residual_norm_backward")
     return g
+
+
+def _seq(t, name, shape, dtype, device):
+    """The distances of consecutive steps and of sequences of a [L, B, d]
+    tensor with contiguous features."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if not (t.is_cuda or sru._on_gpu(t)):
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    st, sb, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"{name} must have contiguous features")
+    return st, sb
+
+
+def _lru_inputs(x, r, i, lam, mask, reset):
+    """Checked inputs: (L, B, d), code, device, and the distances of x, r, i."""
+    code = _dtype(x, "x")
+    if x.dim() != 3:
+        raise ValueError("x must be a 3-d tensor [L, B, d]")
+    dv = _here(x, "x")
+    shape = x.shape
+    L, B, d = shape
+    steps = (_seq(x, "x", shape, x.dtype, dv), _seq(r, "r", shape, x.dtype, dv),
+             _seq(i, "i", shape, x.dtype, dv))
+    _req(lam, "lam", (d,), device=dv)
+    _req(mask, "mask", (L, B), dtype=torch.uint8, optional=True, device=dv)
+    _req(reset, "reset", (L, B), dtype=torch.uint8, optional=True, device=dv)
+    return shape, code, dv, steps
+
+
+def _seq_out(out, name, shape, dtype, device):
+    """(out[name] or a new tensor, its distances)."""
+    t = None if out is None else out.get(name)
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=device)
+    return t, _seq(t, name, shape, dtype, device)
+
+
+def lru_forward(x, r, i, lam, h0=None, mask=None, reset=None, c=8.0, keep_states=True, out=None,
+                ws=None):
+    """Gated linear recurrence over the first dimension of x, r, i [L, B, d]:
+
+        a = exp(-c softplus(lam) sigma(r)),  h_t = a h_{t-1} + sqrt(1 - a^2) sigma(i) x
+
+    lam [d]; h0 [B, d] float32 (None: zeros); mask [L, B] uint8, nonzero where a
+    step is padded (the state passes, the output is 0); reset [L, B] uint8,
+    nonzero where a new document starts (a = 0).  Returns dict(H [L, B, d],
+    h_last [B, d], states): states, the state before every LRU_STEPS-th step,
+    is what lru_backward needs (None with keep_states=False).  x, r, i and H
+    may be strided: slices of one projection, or [B, L, d] transposed."""
+    shape, code, dv, (sx, sr, si) = _lru_inputs(x, r, i, lam, mask, reset)
+    L, B, d = shape
+    _req(h0, "h0", (B, d), optional=True, device=dv)
+    H, sh = _seq_out(out, "H", shape, x.dtype, dv)
+    h_last = _out(out, "h_last", (B, d), _F32, dv)
+    states = (_out(out, "states", (-(-L // LRU_STEPS), B, d), _F32, dv) if keep_states else None)
+    lib = sru.lib()
+    ws, nbytes = _ws(ws, lib.sru_lru_forward_workspace_bytes(L, B, d) if L > LRU_SEGMENT else 0, dv)
+    st = lib.sru_lru_forward(L, B, d, code, _ptr(x), *sx, _ptr(r), *sr, _ptr(i), *si, _ptr(lam), c,
+                             _ptr(h0), _ptr(mask), _ptr(reset), _ptr(H), *sh, _ptr(h_last),
+                             _ptr(states), _ptr(ws), nbytes, sru._stream())
+    _check(st, "sru_lru_forward")
+    return dict(H=H, h_last=h_last, states=states)
+
+
+def lru_backward(x, r, i, lam, states, dH, dh_last=None, mask=None, reset=None, c=8.0,
+                 want_dh0=True, out=None, ws=None):
+    """Gradients of lru_forward given its inputs, its states and the gradients
+    dH [L, B, d] of H and dh_last [B, d] of h_last: dict(dx, dr, di, dlam, dh0).
+    out may hold any of them (dx, dr, di as slices of one tensor)."""
+    shape, code, dv, (sx, sr, si) = _lru_inputs(x, r, i, lam, mask, reset)
+    L, B, d = shape
+    _req(states, "states", (-(-L // LRU_STEPS), B, d), device=dv)
+    sdh = _seq(dH, "dH", shape, x.dtype, dv)
+    _req(dh_last, "dh_last", (B, d), optional=True, device=dv)
+    dx, sdx = _seq_out(out, "dx", shape, x.dtype, dv)
+    dr, sdr = _seq_out(out, "dr", shape, x.dtype, dv)
+    di, sdi = _seq_out(out, "di", shape, x.dtype, dv)
+    dlam = _out(out, "dlam", (d,), _F32, dv)
+    dh0 = _out(out, "dh0", (B, d), _F32, dv) if want_dh0 else None
+    lib = sru.lib()
+    ws, nbytes = _ws(ws, lib.sru_lru_backward_workspace_bytes(L, B, d), dv)
+    st = lib.sru_lru_backward(L, B, d, code, _ptr(x), *sx, _ptr(r), *sr, _ptr(i), *si, _ptr(lam),
+                              c, _ptr(states), _ptr(dH), *sdh, _ptr(dh_last), _ptr(mask),
+                              _ptr(reset), _ptr(dx), *sdx, _ptr(dr), *sdr, _ptr(di), *sdi,
+                              _ptr(dlam), _ptr(dh0), _ptr(ws), nbytes, sru._stream())
+    _check(st, "sru_lru_backward")
+    return dict(dx=dx, dr=dr, di=di, dlam=dlam, dh0=dh0)
+
+
+def lru_step(x, r, i, lam, h, c=8.0, out=None):
+    """One token of the recurrence: x, r, i [B, d], the state h [B, d] float32
+    taken on in place.  Returns the output [B, d] (out, or a new tensor)."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a 2-d tensor [B, d]")
+    if h is None:
+        raise ValueError("h is required")
+    one = [t.unsqueeze(0) if isinstance(t, torch.Tensor) else t for t in (x, r, i)]
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    elif not isinstance(out, torch.Tensor):
+        raise ValueError("out must be a torch tensor")
+    lru_forward(*one, lam, h, c=c, keep_states=False, out=dict(H=out.unsqueeze(0), h_last=h))
+    return out

@@ -75,6 +75,12 @@ _SIGNATURES = {
     "sru_residual_norm_backward_workspace_bytes": (_S, [_I] * 2),
     "sru_residual_norm_backward": (_I, [_I] * 5 + [_P, _L] * 3 + [_P] * 4 + [_P, _L] * 5
                                    + [_P] * 3 + [_P, _S, _P]),
+    "sru_lru_forward_workspace_bytes": (_S, [_I] * 3),
+    "sru_lru_forward": (_I, [_I] * 4 + [_P, _L, _L] * 3 + [_P, _F] + [_P] * 3 + [_P, _L, _L]
+                        + [_P] * 2 + [_P, _S, _P]),
+    "sru_lru_backward_workspace_bytes": (_S, [_I] * 3),
+    "sru_lru_backward": (_I, [_I] * 4 + [_P, _L, _L] * 3 + [_P, _F, _P] + [_P, _L, _L]
+                         + [_P] * 3 + [_P, _L, _L] * 3 + [_P] * 2 + [_P, _S, _P]),
     "sru_timing_begin": (_I, [_P, _I]),
     "sru_timing_end": (_I, []),
     "sru_timing_label": (ctypes.c_char_p, [_I]),

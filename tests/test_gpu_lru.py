@@ -1,0 +1,382 @@
+"""The gated linear recurrence on the GPU against a plain step-by-step
+implementation in 64 bits (gradients by automatic differentiation): lengths on
+both sides of a wave's steps and of a segment, odd widths, both orders of L and
+B, padding, new documents, calls cut in two, single tokens.
+
+Tolerances: every decay, gate and root carries a few roundings of 2^-24 (the
+decay's exponent k s up to 2^-23 k s), and a state is a sum of terms each
+damped by the later decays, so it is off by at most (2 + k) 2^-22 of the sum of
+their magnitudes, about 2e-6 (c = 8, softplus(lam) <= 1.4: k <= 11); a gradient
+sums such errors once more over time and through 1 / beta.  1e-5 of the largest
+magnitude of the sequence's channel covers both for the lengths here, where
+sums of magnitudes are within ten times the largest value; the gradient of lam
+is held to 1e-5 of the sum of its terms' magnitudes.  bf16 results add half a
+step, 2^-8 of the value."""
+
+import math
+
+import pytest
+import torch
+
+from paper_1709_02755_amd import lm, sru
+
+pytestmark = pytest.mark.gpu
+
+F32, B16 = torch.float32, torch.bfloat16
+C = 8.0
+
+
+def inputs(L, B, d, dtype, seed, mask=False, reset=False, slow=True):
+    g = torch.Generator().manual_seed(seed)
+
+    def r(*shape):
+        return torch.randn(shape, generator=g)
+
+    u = 0.9 + 0.099 * torch.rand(d, generator=g)
+    lam = torch.log(torch.expm1(-torch.log(u) / C)) if slow else torch.empty(d).uniform_(
+        -2, 1, generator=g)
+    t = dict(x=r(L, B, d).to(dtype), r=r(L, B, d).to(dtype), i=r(L, B, d).to(dtype), lam=lam,
+             h0=r(B, d), dH=r(L, B, d).to(dtype), dh_last=r(B, d), mask=None, reset=None)
+    if mask:
+        m = torch.rand((L, B), generator=g) < 0.2
+        m[:, 0] = False
+        if B > 1:
+            m[:, 1] = True              # nothing of this sequence counts
+        if B > 2:
+            m[L // 2:, 2] = True
+        t["mask"] = m.to(torch.uint8) * 3   # any nonzero value
+    if reset:
+        z = torch.rand((L, B), generator=g) < 0.05
+        z[0, 0] = True
+        t["reset"] = z.to(torch.uint8)
+    return t
+
+
+def plain(t, grad=True):
+    """(H, h_last), the gradients and the magnitude of lam's, in 64 bits."""
+    v = {n: t[n].detach().cpu().double().requires_grad_(grad)
+         for n in ("x", "r", "i", "lam", "h0")}
+    L = v["x"].shape[0]
+    s, g = torch.sigmoid(v["r"]), torch.sigmoid(v["i"])
+    la = -C * torch.nn.functional.softplus(v["lam"]) * s
+    la.retain_grad() if grad else None
+    a = torch.exp(la)
+    beta = torch.sqrt(-torch.expm1(2 * la))
+    h, hs = v["h0"], []
+    for k in range(L):
+        new = a[k] * h + beta[k] * g[k] * v["x"][k]
+        if t["reset"] is not None:
+            z = (t["reset"][k] != 0)[:, None].cpu()
+            new = torch.where(z, g[k] * v["x"][k], new)
+        if t["mask"] is not None:
+            p = (t["mask"][k] != 0)[:, None].cpu()
+            h = torch.where(p, h, new)
+            hs.append(torch.where(p, 0.0, h))
+        else:
+            h = new
+            hs.append(h)
+    H = torch.stack(hs)
+    if not grad:
+        return H, h, None, None
+    total = (H * t["dH"].cpu().double()).sum()
+    if t["dh_last"] is not None:
+        total = total + (h * t["dh_last"].cpu().double()).sum()
+    total.backward()
+    sig = torch.sigmoid(v["lam"].detach())
+    lam_mag = C * sig * (la.grad * s.detach()).abs().sum((0, 1))
+    return H.detach(), h.detach(), {n: a.grad for n, a in v.items()}, lam_mag
+
+
+def close(name, got, ref, scale=None):
+    got = got.detach()
+    bf16 = got.dtype == B16
+    got = got.cpu().double()
+    assert got.shape == ref.shape, name
+    if scale is None:
+        scale = ref.abs()
+        scale = scale.amax(0, keepdim=True) if ref.dim() == 3 else scale
+        scale = scale.clamp(min=1.0)  # values of unit size make these up
+    tol = 1e-5 * scale + (2.0 ** -8 * ref.abs() if bf16 else 0.0)
+    err = (got - ref).abs()
+    assert bool((err <= tol).all()), (name, float((err - tol).max()))
+
+
+def dev(t):
+    return {n: None if a is None else a.cuda() for n, a in t.items()}
+
+
+def forward(t, **kw):
+    return lm.lru_forward(t["x"], t["r"], t["i"], t["lam"], t["h0"], mask=t["mask"],
+                          reset=t["reset"], c=C, **kw)
+
+
+def backward(t, states, **kw):
+    return lm.lru_backward(t["x"], t["r"], t["i"], t["lam"], states, t["dH"], t["dh_last"],
+                           mask=t["mask"], reset=t["reset"], c=C, **kw)
+
+
+def check(t):
+    H, h_last, ref, lam_mag = plain(t)
+    d = dev(t)
+    fw = forward(d)
+    g = backward(d, fw["states"])
+    torch.cuda.synchronize()
+    close("H", fw["H"], H)
+    close("h_last", fw["h_last"], h_last)
+    for n in ("x", "r", "i", "h0"):
+        close("d" + n, g["d" + n], ref[n])
+    close("dlam", g["dlam"], ref["lam"], lam_mag + 1e-30)
+    return fw, g
+
+
+SHAPES = [(1, 1, 1), (1, 3, 64), (2, 2, 7), (7, 1, 130), (8, 5, 33), (9, 2, 64), (63, 3, 40),
+          (127, 2, 65), (128, 1, 128), (129, 3, 66), (256, 4, 96), (300, 33, 129), (1000, 2, 31),
+          (2050, 1, 64), (2304, 2, 128)]
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("L,B,d", SHAPES)
+def test_values_and_gradients(L, B, d, dtype):
+    check(inputs(L, B, d, dtype, L + B + d))
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("mask,reset", [(True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("L,B,d", [(1, 3, 5), (20, 3, 64), (131, 4, 34), (700, 3, 65)])
+def test_padding_and_documents(L, B, d, mask, reset, dtype):
+    check(inputs(L, B, d, dtype, 3 * L + B, mask, reset))
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_fast_decay(dtype):
+    """States that forget within a few steps: products of decays underflow
+    inside a segment, and across it nothing is left."""
+    check(inputs(400, 2, 70, dtype, 5, slow=False))
+
+
+def test_without_the_optional_parts():
+    t = inputs(150, 2, 48, F32, 6)
+    t["h0"], t["dh_last"] = None, None
+    full = dict(t, h0=torch.zeros((2, 48)))
+    H, h_last, ref, lam_mag = plain(full)
+    d = dev(t)
+    fw = forward(d, keep_states=False)
+    assert fw["states"] is None
+    close("H", fw["H"], H)
+    fw = forward(d)
+    g = backward(d, fw["states"], want_dh0=False)
+    assert g["dh0"] is None
+    close("dr", g["dr"], ref["r"])
+    close("dlam", g["dlam"], ref["lam"], lam_mag)
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("L,B,d", [(37, 3, 24), (260, 2, 33)])
+def test_strides(L, B, d, dtype):
+    """Slices of one projection, [B, L, d] memory, odd offsets: the same results,
+    and nothing beside them is touched."""
+    t = inputs(L, B, d, dtype, 8, True, True)
+    v = dev(t)
+    fw, want = forward(v), None
+    want = backward(v, fw["states"])
+
+    def place(a, kind):
+        if kind == "slice":
+            buf = torch.full((L, B, 3 * d + 1), 9.0, dtype=dtype, device="cuda")
+            s = buf[..., d:2 * d]
+        elif kind == "batch":
+            buf = torch.full((B, L, d), 9.0, dtype=dtype, device="cuda")
+            s = buf.transpose(0, 1)
+        else:
+            buf = torch.full((L * B * d + 1,), 9.0, dtype=dtype, device="cuda")
+            s = buf[1:].view(L, B, d)
+        if a is not None:
+            s.copy_(a)
+        return s, buf
+
+    for kind in ("slice", "batch", "offset"):
+        w = dict(v, **{n: place(v[n], kind)[0] for n in ("x", "r", "i", "dH")})
+        H, bufh = place(None, kind)
+        f2 = forward(w, out=dict(H=H))
+        assert f2["H"] is H
+        outs = {n: place(None, kind) for n in ("dx", "dr", "di")}
+        g2 = backward(w, f2["states"], out={n: o[0] for n, o in outs.items()})
+        close("H", H, fw["H"].cpu().double())
+        for n in ("dx", "dr", "di", "dh0"):
+            close(n, g2[n], want[n].cpu().double())
+        close("dlam", g2["dlam"], want["dlam"].cpu().double(),
+              want["dlam"].cpu().double().abs() + 10.0)
+        if kind == "slice":
+            for buf in [bufh] + [o[1] for o in outs.values()]:
+                assert bool((buf[..., :d] == 9).all()) and bool((buf[..., 2 * d:] == 9).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_single_tokens_and_cut_calls(dtype):
+    """Token by token, and in two calls, against one call."""
+    L, B, d = 150, 3, 66
+    t = inputs(L, B, d, dtype, 9)
+    H, h_last, ref, _ = plain(t)
+    v = dev(t)
+    h = v["h0"].clone()
+    rows = [lm.lru_step(v["x"][k], v["r"][k], v["i"][k], v["lam"], h, c=C) for k in range(L)]
+    close("H", torch.stack(rows), H)
+    close("h", h, h_last)
+    cut = 133
+    a, b = ({n: (x[s] if n in ("x", "r", "i", "dH") else x) for n, x in v.items()}
+            for s in (slice(0, cut), slice(cut, L)))
+    fa = forward(a)
+    b["h0"] = fa["h_last"]
+    fb = forward(b)
+    close("H", torch.cat([fa["H"], fb["H"]]), H)
+    gb = backward(b, fb["states"])
+    a["dh_last"] = gb["dh0"]
+    ga = backward(a, fa["states"])
+    close("dx", torch.cat([ga["dx"], gb["dx"]]), ref["x"])
+    close("dh0", ga["dh0"], ref["h0"])
+
+
+def test_what_does_not_count_reaches_nothing():
+    """NaN and infinity at padded steps, in a wholly padded sequence and before a
+    new document."""
+    L, B, d = 300, 3, 40
+    t = inputs(L, B, d, F32, 10)
+    t["mask"] = torch.zeros((L, B), dtype=torch.uint8)
+    t["mask"][5, 0] = t["mask"][200, 0] = 1
+    t["mask"][:, 1] = 1
+    t["reset"] = torch.zeros((L, B), dtype=torch.uint8)
+    t["reset"][250, 2] = 1
+    clean = dev(t)
+    fw = forward(clean)
+    g = backward(clean, fw["states"])
+    for n in ("x", "r", "i", "dH"):
+        t[n] = t[n].clone()
+        t[n][5, 0] = math.nan
+        t[n][200, 0] = math.inf
+        t[n][:, 1] = math.nan
+    bad = dev(t)
+    f2 = forward(bad)
+    g2 = backward(bad, f2["states"])
+    for n in ("H", "h_last", "states"):
+        assert torch.equal(f2[n], fw[n]), n
+    for n in g:
+        assert torch.equal(g2[n], g[n]), n
+    assert torch.equal(f2["h_last"][1], clean["h0"][1])
+    assert bool((g2["dx"][:, 1] == 0).all())
+    # a broken document does not reach the next one, in any of its features
+    t["x"][100, 2] = math.nan
+    f3 = forward(dev(t))
+    assert bool(torch.isnan(f3["H"][100:250, 2]).all())
+    assert torch.equal(f3["H"][250:, 2], fw["H"][250:, 2])
+    assert bool(torch.isfinite(f3["H"][:, :2]).all())
+
+
+def test_extreme_gates():
+    """Gates shut and open beyond fp32's range, decays of 0 and of 1."""
+    L, B, d = 140, 1, 12
+    t = inputs(L, B, d, F32, 12)
+    t["lam"] = torch.tensor([-100.0, -30.0, -9.0, 0.0, 5.0, 40.0] * 2)
+    t["r"][:, :, 6:] = 120.0
+    t["r"][::2, :, :3] = -120.0
+    t["i"][::3] = -150.0
+    fw = forward(dev(t))
+    g = backward(dev(t), fw["states"])
+    H, h_last, _, _ = plain(t, grad=False)
+    close("H", fw["H"], H)
+    close("h_last", fw["h_last"], h_last)
+    for n in g.values():
+        assert bool(torch.isfinite(n).all())
+
+
+def test_gradient_against_differences():
+    t = inputs(19, 2, 6, F32, 13, True, True, slow=False)
+    d = dev(t)
+    g = backward(d, forward(d)["states"])
+    gen = torch.Generator().manual_seed(2)
+
+    def f(v):
+        H, h, _, _ = plain(v, grad=False)
+        return float((H * t["dH"].double()).sum() + (h * t["dh_last"].double()).sum())
+
+    for n in ("x", "r", "i", "lam", "h0"):
+        e = torch.randn(t[n].shape, generator=gen, dtype=torch.float64)
+        up = f({**t, n: t[n].double() + 1e-5 * e})
+        down = f({**t, n: t[n].double() - 1e-5 * e})
+        slope = (up - down) / 2e-5
+        assert abs(slope - float((g["d" + n].cpu().double() * e).sum())) <= 1e-4 * (1 + abs(slope))
+
+
+def test_same_bits_every_time():
+    """Many segments joined in whatever order they run: the states and
+    gradients agree to rounding; one segment: to the bit.  On another stream
+    and in a replayed graph, with other work between."""
+    t = dev(inputs(128, 4, 256, B16, 14, True, True))
+    fw = forward(t)
+    g = backward(t, fw["states"])
+    torch.cuda.synchronize()
+    want = [fw["H"], fw["h_last"]] + [g[n] for n in sorted(g)]
+    want = [w.clone() for w in want]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        f2 = forward(t)
+        g2 = backward(t, f2["states"])
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in
+               zip(want, [f2["H"], f2["h_last"]] + [g2[n] for n in sorted(g2)]))
+    long = inputs(5000, 1, 64, F32, 15, False, True)
+    H, _, ref, lam_mag = plain(long)
+    v = dev(long)
+    forward(v)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hf = forward(v)
+        hg = backward(v, hf["states"])
+    other = dev(inputs(5000, 1, 64, F32, 16))
+    for _ in range(3):
+        forward(other)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        close("H", hf["H"], H)
+        close("dr", hg["dr"], ref["r"])
+        close("dlam", hg["dlam"], ref["lam"], lam_mag)
+
+
+def test_past_32_bits():
+    """Sequences that lie past 2^31 elements."""
+    L, B, d = 140, 3, 64
+    t = dev(inputs(L, B, d, B16, 17))
+    want = forward(t)
+    gap = 1 << 30
+    buf = torch.zeros((2 * gap + L * d,), dtype=B16, device="cuda")
+    x = buf.as_strided((L, B, d), (d, gap, 1))
+    x.copy_(t["x"])
+    fw = forward(dict(t, x=x))
+    assert torch.equal(fw["H"], want["H"])
+    g = backward(t, want["states"])
+    g2 = backward(dict(t, x=x), fw["states"], out=dict(dx=x))
+    assert torch.equal(x, g["dx"]) and torch.equal(g2["dr"], g["dr"])
+
+
+def test_refusals():
+    t = dev(inputs(5, 2, 8, B16, 1))
+    x, lam = t["x"], t["lam"]
+    bad = [dict(x=x.half()), dict(x=x[0]), dict(r=t["r"].float()), dict(i=t["i"][:4]),
+           dict(lam=lam[:3]), dict(lam=lam.bfloat16()), dict(h0=t["h0"][:1]),
+           dict(mask=torch.zeros((5, 2), device="cuda")),
+           dict(reset=torch.zeros((2, 5), dtype=torch.uint8, device="cuda")),
+           dict(x=x.transpose(1, 2).contiguous().transpose(1, 2))]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            forward(dict(t, **kw))
+    with pytest.raises(sru.SruError, match="SHAPE"):
+        lm.lru_forward(x, t["r"], t["i"], lam, c=-1.0)
+    with pytest.raises(sru.SruError, match="SHAPE"):
+        lm.lru_forward(x[:0], t["r"][:0], t["i"][:0], lam)
+    with pytest.raises(sru.SruError, match="SHAPE"):
+        forward(t, out=dict(H=torch.empty((1, 2, 8), dtype=B16, device="cuda").expand(5, 2, 8)))
+    with pytest.raises(ValueError):
+        backward(t, torch.zeros((2, 2, 8), device="cuda"))
+    with pytest.raises(ValueError):
+        lm.lru_step(x[0], t["r"][0], t["i"][0], lam, None)
