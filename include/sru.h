@@ -466,14 +466,12 @@ SRU_API int sru_residual_norm_backward(int M, int d, int dtype, int res_dtype, i
  *   states [ceil(L / SRU_LRU_STEPS), B, d]: the state before every
  *     SRU_LRU_STEPS-th step, which the gradient call reads (it reads no H);
  *     NULL in the forward: inference
- * One step with h0 = h_last is the form for single tokens; it needs no
- * workspace, nor does any L <= SRU_LRU_SEGMENT in the forward.  Longer
- * sequences are cut into segments, each one workgroup's, whose maps meet in
+ * One step with h0 = h_last is the form for single tokens.  Sequences of more
+ * than 64 steps are cut into segments, each one workgroup's, whose maps meet in
  * the workspace; the results do not depend on the order in which they ran.
  * A sequence cut into consecutive calls (h_last -> h0) agrees with one call to
  * fp32 rounding. */
 #define SRU_LRU_STEPS 8
-#define SRU_LRU_SEGMENT 128
 SRU_API size_t sru_lru_forward_workspace_bytes(int L, int B, int d);
 SRU_API int sru_lru_forward(int L, int B, int d, int dtype, const void* x, long long x_t,
                             long long x_b, const void* r, long long r_t, long long r_b,

@@ -104,7 +104,8 @@ size_t norm_grad_workspace_bytes(int M, int d);
 hipError_t norm_grad_launch(const NormArgs& a, hipStream_t stream);
 
 // ------------------------------------------------- gated linear recurrence
-constexpr int kLruSteps = 8;  // steps a wave holds; a state is kept for each
+constexpr int kLruSteps = 8;     // a state is kept for so many steps, a wave's of the gradient
+constexpr int kLruForward = 8;   // steps a wave holds in the forward
 
 // [L, B, d] with contiguous features; distances of steps and of sequences in
 // elements.

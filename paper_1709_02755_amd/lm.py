@@ -19,7 +19,7 @@ from .sru import _check, _ptr, _req, _ws
 DTYPE_FP32, DTYPE_BF16 = 0, 1
 MAX_TOP, MAX_TEACHER = 64, 1024
 GATE_SILU, GATE_SIGMOID = 0, 1
-LRU_STEPS, LRU_SEGMENT = 8, 128
+LRU_STEPS = 8
 
 _CODES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
 
@@ -399,7 +399,7 @@ def lru_forward(x, r, i, lam, h0=None, mask=None, reset=None, c=8.0, keep_states
     h_last = _out(out, "h_last", (B, d), _F32, dv)
     states = (_out(out, "states", (-(-L // LRU_STEPS), B, d), _F32, dv) if keep_states else None)
     lib = sru.lib()
-    ws, nbytes = _ws(ws, lib.sru_lru_forward_workspace_bytes(L, B, d) if L > LRU_SEGMENT else 0, dv)
+    ws, nbytes = _ws(ws, lib.sru_lru_forward_workspace_bytes(L, B, d), dv)
     st = lib.sru_lru_forward(L, B, d, code, _ptr(x), *sx, _ptr(r), *sr, _ptr(i), *si, _ptr(lam), c,
                              _ptr(h0), _ptr(mask), _ptr(reset), _ptr(H), *sh, _ptr(h_last),
                              _ptr(states), _ptr(ws), nbytes, sru._stream())

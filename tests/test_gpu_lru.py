@@ -307,40 +307,35 @@ def test_gradient_against_differences():
 
 
 def test_same_bits_every_time():
-    """Many segments joined in whatever order they run: the states and
-    gradients agree to rounding; one segment: to the bit.  On another stream
-    and in a replayed graph, with other work between."""
-    t = dev(inputs(128, 4, 256, B16, 14, True, True))
-    fw = forward(t)
-    g = backward(t, fw["states"])
-    torch.cuda.synchronize()
-    want = [fw["H"], fw["h_last"]] + [g[n] for n in sorted(g)]
-    want = [w.clone() for w in want]
-    side = torch.cuda.Stream()
-    with torch.cuda.stream(side):
-        f2 = forward(t)
-        g2 = backward(t, f2["states"])
-    side.synchronize()
-    assert all(torch.equal(a, b) for a, b in
-               zip(want, [f2["H"], f2["h_last"]] + [g2[n] for n in sorted(g2)]))
-    long = inputs(5000, 1, 64, F32, 15, False, True)
-    H, _, ref, lam_mag = plain(long)
-    v = dev(long)
-    forward(v)
-    torch.cuda.synchronize()
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        hf = forward(v)
-        hg = backward(v, hf["states"])
-    other = dev(inputs(5000, 1, 64, F32, 16))
-    for _ in range(3):
-        forward(other)
+    """One segment and many, in whatever order they run: twice in a row, on
+    another stream and in a replayed graph, with other work between."""
+    for L, B, d, dtype in ((128, 4, 256, B16), (5000, 1, 64, F32), (3000, 3, 130, B16)):
+        t = dev(inputs(L, B, d, dtype, 14, False, True))
+        other = dev(inputs(L, B, d, dtype, 16))
+
+        def step(v):
+            fw = forward(v)
+            g = backward(v, fw["states"])
+            return [fw["H"], fw["h_last"], fw["states"]] + [g[n] for n in sorted(g)]
+
+        want = [w.clone() for w in step(t)]
         torch.cuda.synchronize()
-        graph.replay()
-        torch.cuda.synchronize()
-        close("H", hf["H"], H)
-        close("dr", hg["dr"], ref["r"])
-        close("dlam", hg["dlam"], ref["lam"], lam_mag)
+        assert all(torch.equal(a, b) for a, b in zip(want, step(t)))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = step(t)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held = step(t)
+        for _ in range(3):
+            step(other)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, held))
 
 
 def test_past_32_bits():
