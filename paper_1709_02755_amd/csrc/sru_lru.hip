@@ -31,7 +31,7 @@ namespace sru {
 namespace {
 
 constexpr int T = kLruSteps;
-constexpr int kLook = 16;  // segments of a block
+constexpr int kLook = 8;   // segments of a block
 constexpr int kFewChannels = 4096;
 constexpr float kTiny = 1.17549435e-38f;
 constexpr float kLog2e = 1.44269504088896341f;

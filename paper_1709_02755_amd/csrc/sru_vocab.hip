@@ -179,46 +179,128 @@ __device__ __forceinline__ bool top_better(unsigned k, unsigned i, unsigned k2, 
   return k > k2 || (k == k2 && i < i2);
 }
 
-// A wave's best K: lane l holds the l-th.  Empty places have key 0, below that
-// of any number.
-struct TopList {
-  unsigned key = 0, idx = 0xffffffffu;  // this lane's entry
-  unsigned tk = 0, ti = 0xffffffffu;    // the K-th, uniform
-  __device__ __forceinline__ void insert(unsigned k, unsigned i, int K) {
-    const int pos = __popcll(__ballot(top_better(key, idx, k, i)));
-    const int lane = threadIdx.x & 63;
-    const unsigned pk = __shfl_up(key, 1), pi = __shfl_up(idx, 1);
-    if (lane > pos) {
-      key = pk;
-      idx = pi;
-    } else if (lane == pos) {
-      key = k;
-      idx = i;
+// The largest of a wave's values, by cross-lane moves within rows of 16 lanes,
+// then across rows.
+__device__ __forceinline__ unsigned wave_max(unsigned x) {
+#define SRU_STEP(ctrl, rows) \
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false))
+  SRU_STEP(0x111, 0xf);  // row_shr:1
+  SRU_STEP(0x112, 0xf);  // row_shr:2
+  SRU_STEP(0x114, 0xf);  // row_shr:4
+  SRU_STEP(0x118, 0xf);  // row_shr:8
+  SRU_STEP(0x142, 0xa);  // row_bcast:15
+  SRU_STEP(0x143, 0xc);  // row_bcast:31
+#undef SRU_STEP
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// A wave's 64 keys, the largest in lane 0.
+__device__ __forceinline__ unsigned wave_sort(unsigned key) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int size = 2; size <= 64; size <<= 1) {
+#pragma unroll
+    for (int step = size >> 1; step > 0; step >>= 1) {
+      const unsigned o = __shfl_xor(key, step);
+      const bool larger = ((lane & size) == 0) == ((lane & step) == 0);
+      key = larger ? max(key, o) : min(key, o);
     }
-    tk = __builtin_amdgcn_readlane(key, K - 1);
-    ti = __builtin_amdgcn_readlane(idx, K - 1);
   }
-  // Candidates of the wave's lanes, one each where ok: whatever the others do
-  // to the list, each better one than its K-th goes in.
-  __device__ __forceinline__ void offer(bool ok, unsigned k, unsigned i, int K) {
-    while (true) {
-      const unsigned long long b = __ballot(ok && top_better(k, i, tk, ti));
-      if (!b) break;
-      const int src = __ffsll((long long)b) - 1;
-      insert(__builtin_amdgcn_readlane(k, src), __builtin_amdgcn_readlane(i, src), K);
-      ok = ok && (int)(threadIdx.x & 63) != src;
+  return key;
+}
+
+// Candidates for a row's best K, found by one of a workgroup's W waves: in its
+// LDS, unsorted, all that may be among them.  Mostly few are found: the lanes'
+// best values so far bound them from below (K of a wave's lanes have a value as
+// good as the K-th best of these; so have K / W lanes of every wave, by the
+// least of the waves' K / W-th best), and the bounds are taken anew whenever
+// twice as much has been read.  Where the list fills up all the same (values
+// that rise along the row, or are all alike) it is cut to its best K.
+constexpr int kFoundRest = 128;  // room beyond the candidates of one load
+template <int W>
+struct Found {
+  uint2* list;
+  unsigned* floor;   // LDS, one word for the workgroup: K values have this key or a better one
+  unsigned* bounds;  // LDS, a word for each wave
+  int K;
+  int n = 0;
+  unsigned tk = 0, ti = 0xffffffffu;  // the K-th entry when the list was cut last
+  unsigned best = 0;                  // this lane's best key
+
+  __device__ __forceinline__ void raise(unsigned key) {
+    if ((threadIdx.x & 63) == 0 && key) atomicMax(floor, key);
+  }
+  // by all waves together
+  __device__ __forceinline__ void bound() {
+    const unsigned sorted = wave_sort(best);
+    if ((threadIdx.x & 63) == 0)
+      bounds[threadIdx.x >> 6] = __builtin_amdgcn_readlane(sorted, (K - 1) / W);
+    raise(__builtin_amdgcn_readlane(sorted, K - 1));
+    __syncthreads();
+    unsigned least = bounds[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) least = min(least, bounds[w]);
+    raise(least);
+    __syncthreads();
+  }
+
+  // values f of columns col .. (none where col is past V)
+  template <int VE>
+  __device__ __forceinline__ void take(const float (&f)[VE], float vmax, unsigned col, unsigned V) {
+    const unsigned shared = *(volatile unsigned*)floor;
+    if (!__any(top_key(vmax) >= max(tk, shared))) return;
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      const unsigned key = top_key(f[j]), at = col + j;
+      const bool ok = f[j] == f[j] && key >= shared && at < V && top_better(key, at, tk, ti);
+      const unsigned long long b = __ballot(ok);
+      if (ok)
+        list[n + __builtin_amdgcn_mbcnt_hi((unsigned)(b >> 32),
+                                           __builtin_amdgcn_mbcnt_lo((unsigned)b, 0))] =
+            make_uint2(key, at);
+      n += __popcll(b);
     }
+    if (n > kFoundRest) cut();
+  }
+  __device__ __forceinline__ void cut() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int lane = threadIdx.x & 63;
+    for (int e = 0; e < n; e += 64) {
+      const uint2 x = list[min(e + lane, n - 1)];
+      int rank = 0;
+      for (int i = 0; i < n; ++i) {
+        const uint2 y = list[i];
+        rank += top_better(y.x, y.y, x.x, x.y);
+      }
+      const unsigned long long b = __ballot(e + lane < n && rank == K - 1);
+      if (b) {
+        tk = __builtin_amdgcn_readlane(x.x, __ffsll((long long)b) - 1);
+        ti = __builtin_amdgcn_readlane(x.y, __ffsll((long long)b) - 1);
+      }
+    }
+    int kept = 0;
+    for (int e = 0; e < n; e += 64) {
+      const uint2 x = list[min(e + lane, n - 1)];
+      const bool ok = e + lane < n && !top_better(tk, ti, x.x, x.y);
+      const unsigned long long b = __ballot(ok);
+      // at or before the place it was read from, which the wave is past
+      if (ok)
+        list[kept + __builtin_amdgcn_mbcnt_hi((unsigned)(b >> 32),
+                                              __builtin_amdgcn_mbcnt_lo((unsigned)b, 0))] = x;
+      kept += __popcll(b);
+    }
+    n = kept;
+    raise(tk);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 };
 
 // -------------------------------------------------------------- one row part
-// Statistics (and the wave's best alternatives) of a part of a row.  `floor`
-// (LDS, one word, 0 before) holds the best K-th key that any wave has: K
-// values are at least that good, so nothing below it is looked at.
+// Statistics of a part of a row, and the wave's candidates for its alternatives.
 template <bool BF16, int THREADS, int U, bool ENT, bool TOP>
 __device__ __forceinline__ Run<ENT> part_stats(const typename Elem<BF16>::T* z, int V, int part,
-                                               int parts, float k, int K, unsigned* floor,
-                                               TopList& top) {
+                                               int parts, float k,
+                                               Found<THREADS / 64>& top) {
   using E = Elem<BF16>;
   constexpr int VE = E::VE;
   const Span sp = row_span<BF16>(z, V);
@@ -233,20 +315,10 @@ __device__ __forceinline__ Run<ENT> part_stats(const typename Elem<BF16>::T* z, 
 #pragma unroll
     for (int j = 1; j < VE; ++j) vm = fmaxf(vm, f[j]);
     run.add(f, vm, k);
-    if constexpr (TOP) {
-      const unsigned shared = *(volatile unsigned*)floor;
-      if (__any(top_key(vm) >= max(top.tk, shared))) {
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-          const unsigned key = top_key(f[j]);
-          // places past the part's end are -inf with a column that is none
-          top.offer(f[j] == f[j] && key >= shared && col + j < (unsigned)V, key, col + j, K);
-        }
-        if (top.tk > shared && (tid & 63) == 0) atomicMax(floor, top.tk);
-      }
-    }
+    if constexpr (TOP) top.take(f, vm, col, (unsigned)V);
   };
 
+  int again = 1;  // rounds until the bounds are taken anew
   for (int v = v0; v < v1; v += THREADS * U) {
     uint4 u[U];
 #pragma unroll
@@ -254,6 +326,24 @@ __device__ __forceinline__ Run<ENT> part_stats(const typename Elem<BF16>::T* z, 
       const int at = v + i * THREADS + tid;
       u[i] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
       if (at < v1) u[i] = zv[at];
+    }
+    if constexpr (TOP) {
+      float vm = -INFINITY;
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (v + i * THREADS + tid < v1) {
+          float f[VE];
+          E::unpack(u[i], f);
+#pragma unroll
+          for (int j = 0; j < VE; ++j) vm = fmaxf(vm, f[j]), any |= f[j] == f[j];
+        }
+      }
+      if (any) top.best = max(top.best, top_key(vm));
+      if (--again == 0) {
+        top.bound();
+        again = (v - v0) / (THREADS * U) + 1;
+      }
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -274,37 +364,87 @@ __device__ __forceinline__ Run<ENT> part_stats(const typename Elem<BF16>::T* z, 
     if (col >= 0) f[0] = E::get(z[col]);
     float vm = f[0];
     run.add(f, vm, k);
-    if constexpr (TOP)
-      top.offer(col >= 0 && vm == vm && top_key(vm) >= *(volatile unsigned*)floor, top_key(vm),
-                (unsigned)col, K);
+    if constexpr (TOP) {
+      // the other places of the vector are no columns
+#pragma unroll
+      for (int j = 1; j < VE; ++j) f[j] = NAN;
+      top.take(f, vm, col >= 0 ? (unsigned)col : 0x80000000u, (unsigned)V);
+    }
   }
   return run;
 }
 
-// The best K of n lists of K (key, column) pairs each, best first, in LDS:
-// every entry's rank is the number of entries that are better, found in each
-// other list by halving.  put(rank, key, column) for the K best.
+// The best K of what a workgroup's waves have found, n[w] entries in list w (of
+// pitch `pitch`), in order: put(rank, key, column) for each, and for the places
+// that nothing fills (key 0).  What is below the last bound is dropped first
+// (into `kept`, LDS, at most `room` entries; with more, all are ranked).
 template <int THREADS, typename F>
-__device__ __forceinline__ void top_merge(const uint2* lists, int n, int K, F put) {
-  for (int e = threadIdx.x; e < n * K; e += THREADS) {
-    const uint2 x = lists[e];
-    const int mine = e / K;
-    int rank = e - mine * K;
-    for (int l = 0; l < n && rank < K; ++l) {
-      if (l == mine) continue;
-      int lo = 0, hi = K;  // entries before lo are better than x
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        const uint2 y = lists[l * K + mid];
-        // empty places are all alike: those of earlier lists come first
-        const bool better = top_better(y.x, y.y, x.x, x.y) ||
-                            (y.x == x.x && y.y == x.y && l < mine);
-        if (better) lo = mid + 1;
-        else hi = mid;
-      }
-      rank += lo;
+__device__ __forceinline__ void top_merge(const uint2* lists, int pitch, const int* n,
+                                          unsigned floor, int K, uint2* kept, int room,
+                                          int* kept_n, F put) {
+  constexpr int W = THREADS / 64;
+  int total = 0;
+  for (int w = 0; w < W; ++w) total += n[w];
+  if (threadIdx.x == 0) *kept_n = 0;
+  __syncthreads();
+  for (int e = threadIdx.x; e < total; e += THREADS) {
+    int w = 0, i = e;
+    while (i >= n[w]) i -= n[w++];
+    const uint2 x = lists[w * pitch + i];
+    if (x.x < floor) continue;  // K others are better
+    const int to = atomicAdd(kept_n, 1);
+    if (to < room) kept[to] = x;
+  }
+  __syncthreads();
+  const int some = *kept_n;
+  if (some <= room) {
+    // in any order: a rank depends on the entries alone
+    for (int e = threadIdx.x; e < some; e += THREADS) {
+      const uint2 x = kept[e];
+      int rank = 0;
+      for (int i = 0; i < some; ++i) rank += top_better(kept[i].x, kept[i].y, x.x, x.y);
+      if (rank < K) put(rank, x.x, x.y);
     }
-    if (rank < K) put(rank, x.x, x.y);
+  } else {
+    for (int e = threadIdx.x; e < total; e += THREADS) {
+      int w = 0, i = e;
+      while (i >= n[w]) i -= n[w++];
+      const uint2 x = lists[w * pitch + i];
+      int rank = 0;
+      for (int l = 0; l < W && rank < K; ++l)
+        for (int q = 0; q < n[l]; ++q) {
+          const uint2 y = lists[l * pitch + q];
+          rank += top_better(y.x, y.y, x.x, x.y);
+        }
+      if (rank < K) put(rank, x.x, x.y);
+    }
+  }
+  for (int r = total + threadIdx.x; r < K; r += THREADS) put(r, 0u, 0xffffffffu);
+}
+
+// The best K of up to 64 lists of K entries, best first, by one wave, a lane a
+// list: K times the best of the lists' first entries is taken off.  next(list, entry) reads an entry.
+template <typename N, typename F>
+__device__ __forceinline__ void top_take(int n, int K, N next, F put) {
+  const int lane = threadIdx.x & 63;
+  int at = 0;
+  uint2 x = lane < n ? next(lane, 0) : make_uint2(0u, 0xffffffffu);
+  for (int k = 0; k < K; ++k) {
+    const unsigned key = wave_max(x.x);
+    unsigned long long b = __ballot(x.x == key && lane < n);
+    int win = __ffsll((long long)b) - 1;
+    unsigned idx = __builtin_amdgcn_readlane(x.y, win);
+    // equal values: the lowest column
+    while (b &= b - 1) {
+      const int l = __ffsll((long long)b) - 1;
+      const unsigned i = __builtin_amdgcn_readlane(x.y, l);
+      if (i < idx) idx = i, win = l;
+    }
+    if (lane == win) {
+      put(k, key, idx);
+      ++at;
+      x = at < K ? next(lane, at) : make_uint2(0u, 0xffffffffu);
+    }
   }
 }
 
@@ -350,66 +490,69 @@ __device__ __forceinline__ void top_write(const LogprobArgs& a, int row, const R
 // floats, then [row, part, K] pairs.
 template <bool BF16, int THREADS, int U, bool TOP>
 __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a, int parts) {
-  constexpr int W = THREADS / 64;
-  __shared__ float red[3 * W];
-  __shared__ unsigned floor;
-  __shared__ uint2 lists[TOP ? W * kMaxTop : 1];
   using E = Elem<BF16>;
+  constexpr int W = THREADS / 64, kPitch = 64 * E::VE + kFoundRest;
+  __shared__ float red[3 * W];
+  constexpr int kRoom = TOP ? 512 : 1;
+  __shared__ unsigned floor, bounds[W];
+  __shared__ int count[W], kept_n;
+  __shared__ uint2 lists[TOP ? W * kPitch : 1], kept[kRoom];
+  const int wave = threadIdx.x >> 6;
   const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
   const long long items = (long long)a.r.N * parts;
   for (long long it = blockIdx.x; it < items; it += gridDim.x) {
     const int row = (int)(it / parts), part = (int)(it - (long long)row * parts);
     const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
-    TopList top;
+    Found<W> top{lists + (TOP ? wave * kPitch : 0), &floor, bounds, a.top};
     if constexpr (TOP) {
       if (threadIdx.x == 0) floor = 0;
       __syncthreads();
     }
-    Run<true> run = part_stats<BF16, THREADS, U, true, TOP>(z, a.r.V, part, parts, k, a.top,
-                                                            &floor, top);
+    Run<true> run = part_stats<BF16, THREADS, U, true, TOP>(z, a.r.V, part, parts, k, top);
     if constexpr (TOP) {
-      const int lane = threadIdx.x & 63;
-      if (lane < a.top) lists[(threadIdx.x >> 6) * a.top + lane] = make_uint2(top.key, top.idx);
+      if ((threadIdx.x & 63) == 0) count[wave] = top.n;
     }
     run = run_block<THREADS>(run, k, red);  // its barriers make the lists visible
     if (parts == 1) {
       if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
       if constexpr (TOP) {
         const RowStats st = row_stats(run.m, run.s);
-        top_merge<THREADS>(lists, W, a.top, [&](int rank, unsigned key, unsigned idx) {
-          top_write(a, row, st, inv_t, rank, key, idx);
-        });
+        top_merge<THREADS>(lists, kPitch, count, floor, a.top, kept, kRoom, &kept_n,
+                           [&](int rank, unsigned key, unsigned idx) {
+                             top_write(a, row, st, inv_t, rank, key, idx);
+                           });
       }
     } else {
       float* ws = static_cast<float*>(a.workspace);
       if (threadIdx.x == 0) run_store(ws + 4 * it, run);
       if constexpr (TOP) {
         uint2* wl = reinterpret_cast<uint2*>(ws + 4 * items) + it * a.top;
-        top_merge<THREADS>(lists, W, a.top, [&](int rank, unsigned key, unsigned idx) {
-          wl[rank] = make_uint2(key, idx);
-        });
+        top_merge<THREADS>(lists, kPitch, count, floor, a.top, kept, kRoom, &kept_n,
+                           [&](int rank, unsigned key, unsigned idx) {
+                             wl[rank] = make_uint2(key, idx);
+                           });
       }
     }
-    __syncthreads();  // lists and floor are used again
+    __syncthreads();  // lists, count and floor are used again
   }
 }
 
 constexpr int kMaxParts = 64;
 
-// The parts of a row joined, one workgroup per row.
+// The parts of a row joined: one wave a row, a lane a part.
 template <bool BF16, bool TOP>
-__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int parts) {
+__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a, int parts) {
   extern __shared__ uint2 lists[];
   const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
   const float* ws = static_cast<const float*>(a.workspace);
   const uint2* wl = reinterpret_cast<const uint2*>(ws + 4LL * a.r.N * parts);
+  const int lane = threadIdx.x;
   for (int row = blockIdx.x; row < a.r.N; row += gridDim.x) {
     if constexpr (TOP) {
-      for (int e = threadIdx.x; e < parts * a.top; e += 256)
+      __syncthreads();  // the lists' earlier use
+      for (int e = lane; e < parts * a.top; e += 64)
         lists[e] = wl[(long long)row * parts * a.top + e];
     }
-    // one part a lane, joined across the wave; every wave does the same
-    const int lane = threadIdx.x & 63;
     Run<true> run;
     if (lane < parts) run = run_load<true>(ws + 4 * ((long long)row * parts + lane));
 #pragma unroll
@@ -420,14 +563,15 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int pa
       b.t = __shfl_xor(run.t, o);
       run.join(b, k);
     }
-    if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
+    if (lane == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
     if constexpr (TOP) {
       __syncthreads();
       const RowStats st = row_stats(run.m, run.s);
-      top_merge<256>(lists, parts, a.top, [&](int rank, unsigned key, unsigned idx) {
-        top_write(a, row, st, inv_t, rank, key, idx);
-      });
-      __syncthreads();
+      top_take(
+          parts, a.top, [&](int l, int e) { return lists[l * a.top + e]; },
+          [&](int rank, unsigned key, unsigned idx) {
+            top_write(a, row, st, inv_t, rank, key, idx);
+          });
     }
   }
 }
@@ -673,9 +817,8 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int par
     const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
     float m, s;
     if constexpr (STATS) {
-      TopList none;
-      Run<false> run = part_stats<BF16, THREADS, U, false, false>(z, a.r.V, part, parts, k, 0,
-                                                                  nullptr, none);
+      Found<W> none{nullptr, nullptr, nullptr, 0};
+      Run<false> run = part_stats<BF16, THREADS, U, false, false>(z, a.r.V, part, parts, k, none);
       run = run_block<THREADS>(run, k, red);
       m = run.m;
       s = run.s;
@@ -755,9 +898,10 @@ constexpr int kThreads = 512;
 constexpr int kUnroll = 4;
 
 // Parts a row is cut into: with fewer rows than CUs some would have nothing to
-// do, but a part has at least one round of vectors.
-int row_parts(int N, int V, bool bf16) {
-  const int round = kThreads * (bf16 ? 8 : 4);
+// do, but a part has at least one round of vectors (with alternatives, whose
+// lists have to be filled in every part, one for every load in flight).
+int row_parts(int N, int V, bool bf16, bool top = false) {
+  const int round = kThreads * (bf16 ? 8 : 4) * (top ? kUnroll : 1);
   const int want = (512 + N - 1) / N, most = (V + round - 1) / round;
   const int p = want < most ? want : most;
   return p < 1 ? 1 : p > kMaxParts ? kMaxParts : p;
@@ -766,7 +910,7 @@ dim3 grid_of(long long items) { return dim3((unsigned)(items < kMaxGrid ? items 
 
 template <bool BF16, bool TOP>
 hipError_t logprob_run(const LogprobArgs& a, hipStream_t st) {
-  const int parts = row_parts(a.r.N, a.r.V, BF16);
+  const int parts = row_parts(a.r.N, a.r.V, BF16, TOP);
   timing_before("logprobs", st);
   hipLaunchKernelGGL((logprob_kernel<BF16, kThreads, kUnroll, TOP>),
                      grid_of((long long)a.r.N * parts), dim3(kThreads), 0, st, a, parts);
@@ -774,7 +918,7 @@ hipError_t logprob_run(const LogprobArgs& a, hipStream_t st) {
   if (hipError_t e = hipGetLastError()) return e;
   if (parts == 1) return hipSuccess;
   timing_before("logprobs_join", st);
-  hipLaunchKernelGGL((logprob_join_kernel<BF16, TOP>), grid_of(a.r.N), dim3(256),
+  hipLaunchKernelGGL((logprob_join_kernel<BF16, TOP>), grid_of(a.r.N), dim3(64),
                      TOP ? sizeof(uint2) * parts * a.top : 0, st, a, parts);
   timing_after(st);
   return hipGetLastError();
@@ -811,7 +955,7 @@ hipError_t distill_run(const DistillArgs& a, hipStream_t st) {
 }  // namespace
 
 size_t logprob_workspace_bytes(int N, int V, int bf16, int top) {
-  const int parts = row_parts(N, V, bf16 != 0);
+  const int parts = row_parts(N, V, bf16 != 0, top > 0);
   return parts == 1 ? 0 : (size_t)N * parts * (16 + sizeof(uint2) * top);
 }
 
