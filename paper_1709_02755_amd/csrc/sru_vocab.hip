@@ -179,21 +179,6 @@ __device__ __forceinline__ bool top_better(unsigned k, unsigned i, unsigned k2, 
   return k > k2 || (k == k2 && i < i2);
 }
 
-// The largest of a wave's values, by cross-lane moves within rows of 16 lanes,
-// then across rows.
-__device__ __forceinline__ unsigned wave_max(unsigned x) {
-#define SRU_STEP(ctrl, rows) \
-  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false))
-  SRU_STEP(0x111, 0xf);  // row_shr:1
-  SRU_STEP(0x112, 0xf);  // row_shr:2
-  SRU_STEP(0x114, 0xf);  // row_shr:4
-  SRU_STEP(0x118, 0xf);  // row_shr:8
-  SRU_STEP(0x142, 0xa);  // row_bcast:15
-  SRU_STEP(0x143, 0xc);  // row_bcast:31
-#undef SRU_STEP
-  return __builtin_amdgcn_readlane(x, 63);
-}
-
 // A wave's 64 keys, the largest in lane 0.
 __device__ __forceinline__ unsigned wave_sort(unsigned key) {
   const int lane = threadIdx.x & 63;
@@ -310,10 +295,13 @@ __device__ __forceinline__ Run<ENT> part_stats(const typename Elem<BF16>::T* z, 
   const uint4* zv = reinterpret_cast<const uint4*>(z + sp.head);
   Run<ENT> run;
 
-  auto take = [&](const float(&f)[VE], unsigned col) {
+  auto largest = [](const float(&f)[VE]) {
     float vm = f[0];
 #pragma unroll
     for (int j = 1; j < VE; ++j) vm = fmaxf(vm, f[j]);
+    return vm;
+  };
+  auto take = [&](const float(&f)[VE], float vm, unsigned col) {
     run.add(f, vm, k);
     if constexpr (TOP) top.take(f, vm, col, (unsigned)V);
   };
@@ -327,30 +315,26 @@ __device__ __forceinline__ Run<ENT> part_stats(const typename Elem<BF16>::T* z, 
       u[i] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
       if (at < v1) u[i] = zv[at];
     }
-    if constexpr (TOP) {
-      float vm = -INFINITY;
-      bool any = false;
+    float vm[U];
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        if (v + i * THREADS + tid < v1) {
-          float f[VE];
-          E::unpack(u[i], f);
-#pragma unroll
-          for (int j = 0; j < VE; ++j) vm = fmaxf(vm, f[j]), any |= f[j] == f[j];
-        }
-      }
-      if (any) top.best = max(top.best, top_key(vm));
-      if (--again == 0) {
-        top.bound();
-        again = (v - v0) / (THREADS * U) + 1;
-      }
+    for (int i = 0; i < U; ++i) {
+      float f[VE];
+      E::unpack(u[i], f);
+      vm[i] = largest(f);
+      // (a NaN among others does not show in their largest, and alone is none)
+      if (TOP && v + i * THREADS + tid < v1 && vm[i] == vm[i])
+        top.best = max(top.best, top_key(vm[i]));
+    }
+    if (TOP && --again == 0) {
+      top.bound();
+      again = (v - v0) / (THREADS * U) + 1;
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int at = v + i * THREADS + tid;
       float f[VE];
       E::unpack(u[i], f);
-      take(f, at < v1 ? (unsigned)(sp.head + at * VE) : 0x80000000u);
+      take(f, vm[i], at < v1 ? (unsigned)(sp.head + at * VE) : 0x80000000u);
     }
   }
   // the head and the tail, at most VE - 1 elements each, one a lane
@@ -362,7 +346,7 @@ __device__ __forceinline__ Run<ENT> part_stats(const typename Elem<BF16>::T* z, 
 #pragma unroll
     for (int j = 0; j < VE; ++j) f[j] = -INFINITY;
     if (col >= 0) f[0] = E::get(z[col]);
-    float vm = f[0];
+    const float vm = f[0];
     run.add(f, vm, k);
     if constexpr (TOP) {
       // the other places of the vector are no columns
@@ -374,17 +358,16 @@ __device__ __forceinline__ Run<ENT> part_stats(const typename Elem<BF16>::T* z, 
   return run;
 }
 
-// The best K of what a workgroup's waves have found, n[w] entries in list w (of
-// pitch `pitch`), in order: put(rank, key, column) for each, and for the places
-// that nothing fills (key 0).  What is below the last bound is dropped first
+// The best K of several lists, n[l] entries in list l (of pitch `pitch`), in
+// order: put(rank, key, column) for each, and for the places that nothing fills
+// (key 0).  What is below the last bound is dropped first
 // (into `kept`, LDS, at most `room` entries; with more, all are ranked).
 template <int THREADS, typename F>
-__device__ __forceinline__ void top_merge(const uint2* lists, int pitch, const int* n,
+__device__ __forceinline__ void top_merge(const uint2* lists, int pitch, int count, const int* n,
                                           unsigned floor, int K, uint2* kept, int room,
                                           int* kept_n, F put) {
-  constexpr int W = THREADS / 64;
   int total = 0;
-  for (int w = 0; w < W; ++w) total += n[w];
+  for (int l = 0; l < count; ++l) total += n[l];
   if (threadIdx.x == 0) *kept_n = 0;
   __syncthreads();
   for (int e = threadIdx.x; e < total; e += THREADS) {
@@ -411,7 +394,7 @@ __device__ __forceinline__ void top_merge(const uint2* lists, int pitch, const i
       while (i >= n[w]) i -= n[w++];
       const uint2 x = lists[w * pitch + i];
       int rank = 0;
-      for (int l = 0; l < W && rank < K; ++l)
+      for (int l = 0; l < count && rank < K; ++l)
         for (int q = 0; q < n[l]; ++q) {
           const uint2 y = lists[l * pitch + q];
           rank += top_better(y.x, y.y, x.x, x.y);
@@ -420,32 +403,6 @@ __device__ __forceinline__ void top_merge(const uint2* lists, int pitch, const i
     }
   }
   for (int r = total + threadIdx.x; r < K; r += THREADS) put(r, 0u, 0xffffffffu);
-}
-
-// The best K of up to 64 lists of K entries, best first, by one wave, a lane a
-// list: K times the best of the lists' first entries is taken off.  next(list, entry) reads an entry.
-template <typename N, typename F>
-__device__ __forceinline__ void top_take(int n, int K, N next, F put) {
-  const int lane = threadIdx.x & 63;
-  int at = 0;
-  uint2 x = lane < n ? next(lane, 0) : make_uint2(0u, 0xffffffffu);
-  for (int k = 0; k < K; ++k) {
-    const unsigned key = wave_max(x.x);
-    unsigned long long b = __ballot(x.x == key && lane < n);
-    int win = __ffsll((long long)b) - 1;
-    unsigned idx = __builtin_amdgcn_readlane(x.y, win);
-    // equal values: the lowest column
-    while (b &= b - 1) {
-      const int l = __ffsll((long long)b) - 1;
-      const unsigned i = __builtin_amdgcn_readlane(x.y, l);
-      if (i < idx) idx = i, win = l;
-    }
-    if (lane == win) {
-      put(k, key, idx);
-      ++at;
-      x = at < K ? next(lane, at) : make_uint2(0u, 0xffffffffu);
-    }
-  }
 }
 
 struct RowStats {
@@ -517,7 +474,7 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a, int par
       if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
       if constexpr (TOP) {
         const RowStats st = row_stats(run.m, run.s);
-        top_merge<THREADS>(lists, kPitch, count, floor, a.top, kept, kRoom, &kept_n,
+        top_merge<THREADS>(lists, kPitch, W, count, floor, a.top, kept, kRoom, &kept_n,
                            [&](int rank, unsigned key, unsigned idx) {
                              top_write(a, row, st, inv_t, rank, key, idx);
                            });
@@ -527,7 +484,7 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a, int par
       if (threadIdx.x == 0) run_store(ws + 4 * it, run);
       if constexpr (TOP) {
         uint2* wl = reinterpret_cast<uint2*>(ws + 4 * items) + it * a.top;
-        top_merge<THREADS>(lists, kPitch, count, floor, a.top, kept, kRoom, &kept_n,
+        top_merge<THREADS>(lists, kPitch, W, count, floor, a.top, kept, kRoom, &kept_n,
                            [&](int rank, unsigned key, unsigned idx) {
                              wl[rank] = make_uint2(key, idx);
                            });
@@ -539,20 +496,25 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a, int par
 
 constexpr int kMaxParts = 64;
 
-// The parts of a row joined: one wave a row, a lane a part.
+// The parts of a row joined, one workgroup per row.
 template <bool BF16, bool TOP>
-__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a, int parts) {
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int parts) {
   extern __shared__ uint2 lists[];
+  __shared__ int n[kMaxParts], kept_n;
+  __shared__ unsigned floor;
+  constexpr int kRoom = TOP ? 512 : 1;
+  __shared__ uint2 kept[kRoom];
   const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
   const float* ws = static_cast<const float*>(a.workspace);
   const uint2* wl = reinterpret_cast<const uint2*>(ws + 4LL * a.r.N * parts);
-  const int lane = threadIdx.x;
+  const int lane = threadIdx.x & 63;
   for (int row = blockIdx.x; row < a.r.N; row += gridDim.x) {
     if constexpr (TOP) {
       __syncthreads();  // the lists' earlier use
-      for (int e = lane; e < parts * a.top; e += 64)
+      for (int e = threadIdx.x; e < parts * a.top; e += 256)
         lists[e] = wl[(long long)row * parts * a.top + e];
     }
+    // one part a lane, joined across the wave; every wave does the same
     Run<true> run;
     if (lane < parts) run = run_load<true>(ws + 4 * ((long long)row * parts + lane));
 #pragma unroll
@@ -563,15 +525,25 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a, int par
       b.t = __shfl_xor(run.t, o);
       run.join(b, k);
     }
-    if (lane == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
+    if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
     if constexpr (TOP) {
+      // K / parts entries of every list are at least as good as the least of the
+      // lists' K / parts-th
+      if (threadIdx.x == 0) floor = 0xffffffffu;
+      __syncthreads();
+      if (threadIdx.x < parts) {
+        const uint2* l = lists + threadIdx.x * a.top;
+        int filled = a.top;
+        while (filled > 0 && l[filled - 1].x == 0) --filled;
+        n[threadIdx.x] = filled;
+        atomicMin(&floor, l[(a.top - 1) / parts].x);
+      }
       __syncthreads();
       const RowStats st = row_stats(run.m, run.s);
-      top_take(
-          parts, a.top, [&](int l, int e) { return lists[l * a.top + e]; },
-          [&](int rank, unsigned key, unsigned idx) {
-            top_write(a, row, st, inv_t, rank, key, idx);
-          });
+      top_merge<256>(lists, a.top, parts, n, floor, a.top, kept, kRoom, &kept_n,
+                     [&](int rank, unsigned key, unsigned idx) {
+                       top_write(a, row, st, inv_t, rank, key, idx);
+                     });
     }
   }
 }
@@ -918,7 +890,7 @@ hipError_t logprob_run(const LogprobArgs& a, hipStream_t st) {
   if (hipError_t e = hipGetLastError()) return e;
   if (parts == 1) return hipSuccess;
   timing_before("logprobs_join", st);
-  hipLaunchKernelGGL((logprob_join_kernel<BF16, TOP>), grid_of(a.r.N), dim3(64),
+  hipLaunchKernelGGL((logprob_join_kernel<BF16, TOP>), grid_of(a.r.N), dim3(256),
                      TOP ? sizeof(uint2) * parts * a.top : 0, st, a, parts);
   timing_after(st);
   return hipGetLastError();
