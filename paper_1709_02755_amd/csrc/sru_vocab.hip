@@ -20,6 +20,19 @@ constexpr float kLn2 = 0.693147180559945309f;
 // of -inf, or of the type's lowest value at a temperature below 1).
 constexpr float kLowExp = -200.0f;
 
+// Vectors that are not used again: past the caches, which keep what is (the
+// second read of a row whose gradient is written: 4096 x 65536 bf16, loss and
+// gradient, NTMEASURE).
+typedef unsigned Quad __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_last(const uint4* p) {
+  const Quad q = __builtin_nontemporal_load(reinterpret_cast<const Quad*>(p));
+  return make_uint4(q[0], q[1], q[2], q[3]);
+}
+__device__ __forceinline__ void store_last(uint4* p, const uint4& v) {
+  const Quad q = {v.x, v.y, v.z, v.w};
+  __builtin_nontemporal_store(q, reinterpret_cast<Quad*>(p));
+}
+
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <bool BF16>
@@ -576,7 +589,7 @@ __device__ __forceinline__ void part_grad(const typename Elem<BF16>::T* z,
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int at = v + i * THREADS + tid;
-      if (at < v1 && !none) u[i] = zv[at];
+      if (at < v1 && !none) u[i] = load_last(zv + at);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -587,7 +600,7 @@ __device__ __forceinline__ void part_grad(const typename Elem<BF16>::T* z,
 #pragma unroll
         for (int j = 0; j < VE; ++j) f[j] = grad(f[j]);
         if (whole) {
-          dv[at] = E::pack(f);
+          store_last(dv + at, E::pack(f));
         } else {
 #pragma unroll
           for (int j = 0; j < VE; ++j) dz[sp.head + at * VE + j] = E::put(f[j]);
@@ -624,7 +637,8 @@ struct PointTerms {
   using E = Elem<BF16>;
   float value[PER];
   int at[PER];
-  __device__ __forceinline__ void take(const int* cols, const float* w, int n,
+  // logits: of the columns, or nullptr: read from z
+  __device__ __forceinline__ void take(const int* cols, const float* w, const float* logits, int n,
                                        const typename E::T* z, int V, int part, int parts,
                                        float base, float k, float c0, float c1) {
     const bool none = c0 == 0.f && c1 == 0.f;
@@ -643,7 +657,7 @@ struct PointTerms {
           sum += w[q];
         }
       if (first != e) continue;
-      const float x = (E::get(z[c]) - base) * k;
+      const float x = ((logits ? logits[e] : E::get(z[c])) - base) * k;
       const float g = none ? 0.f
                            : exp2_hw(x) * (LIN ? fmaf(c1, fmaxf(x, kLowExp), c0) : c0);
       value[p] = g + sum;
@@ -689,7 +703,7 @@ __global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LogprobGradArgs a
     const float c0 = -(sum + (dh == 0.f ? 0.f : dh * (a.entropy[row] - st.log_s))) * inv_s;
     const float c1 = dh == 0.f ? 0.f : -dh * kLn2 * inv_s;
     PointTerms<BF16, THREADS, kMaxTop + 1, true> pt;
-    pt.take(cols, wts, n, z, a.r.V, part, parts, st.base, k, c0, c1);
+    pt.take(cols, wts, nullptr, n, z, a.r.V, part, parts, st.base, k, c0, c1);
     __syncthreads();  // dz may be z
     if (c1 == 0.f)
       part_grad<BF16, THREADS, U, false>(z, dz, a.r.V, part, parts, st.base, k, c0, 0.f);
@@ -702,65 +716,97 @@ __global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LogprobGradArgs a
 }
 
 // ------------------------------------------------------------------ distillation
-// The teacher's probabilities p = softmax(t / T) over the row's kept entries
-// (ids within the vocabulary, logits above -inf): cols[e], probs[e] in LDS;
-// returns 1 where there is any, else 0.  scratch: THREADS / 64 floats.
-template <int THREADS>
-__device__ __forceinline__ float teacher_probs(const DistillArgs& a, int row, int* cols,
-                                               float* probs, float* scratch, float k) {
-  constexpr int W = THREADS / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float m = -INFINITY;
-  for (int e = threadIdx.x; e < a.K; e += THREADS) {
-    const long long o = (long long)row * a.K + e;
-    const int64_t c = a.ids[o];
-    const float t = a.teacher_bf16 ? Elem<true>::get(static_cast<const uint16_t*>(a.teacher)[o])
-                                   : static_cast<const float*>(a.teacher)[o];
-    const bool kept = c >= 0 && c < a.r.V && t != -INFINITY;
-    cols[e] = kept ? (int)c : -1;
-    probs[e] = t;
-    // a NaN that fmaxf drops comes back in the sum
-    if (kept) m = fmaxf(m, t);
-  }
+// A row's teacher entries, thread e's every THREADS-th from e: fetched before the
+// row is read, so that the student's logits of the ids can be asked for as soon
+// as that has been (an id that is not kept has column -1).
+template <bool BF16, int THREADS>
+struct Teacher {
+  static constexpr int PER = kMaxTeacher / THREADS;
+  int64_t id[PER];
+  float t[PER], z[PER];
+  int col[PER];
+  __device__ __forceinline__ void fetch(const DistillArgs& a, int row) {
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if (lane == 0) scratch[wave] = m;
-  __syncthreads();
-  for (int w = 0; w < W; ++w) m = fmaxf(m, scratch[w]);
-  __syncthreads();
-  float s = 0.f;
-  bool any = false;
-  for (int e = threadIdx.x; e < a.K; e += THREADS) {
-    const bool kept = cols[e] >= 0;
-    const float p = kept ? exp2_hw((probs[e] - m) * k) : 0.f;
-    probs[e] = p;
-    s += p;
-    any |= kept;
+    for (int p = 0; p < PER; ++p) {
+      const int e = p * THREADS + (int)threadIdx.x;
+      if (e >= a.K) break;
+      const long long o = (long long)row * a.K + e;
+      id[p] = a.ids[o];
+      t[p] = a.teacher_bf16 ? Elem<true>::get(static_cast<const uint16_t*>(a.teacher)[o])
+                            : static_cast<const float*>(a.teacher)[o];
+    }
   }
+  __device__ __forceinline__ void gather(const DistillArgs& a, const typename Elem<BF16>::T* row) {
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
-  if (lane == 0) scratch[wave] = s;
-  const int rows_kept = __syncthreads_or(any);
-  s = 0.f;
-  for (int w = 0; w < W; ++w) s += scratch[w];
-  const float inv = 1.f / s;
-  for (int e = threadIdx.x; e < a.K; e += THREADS) probs[e] = cols[e] >= 0 ? probs[e] * inv : 0.f;
-  __syncthreads();
-  return rows_kept ? 1.f : 0.f;
-}
+    for (int p = 0; p < PER; ++p) {
+      const int e = p * THREADS + (int)threadIdx.x;
+      if (e >= a.K) break;
+      const bool kept = id[p] >= 0 && id[p] < a.r.V && t[p] != -INFINITY;
+      col[p] = kept ? (int)id[p] : -1;
+      z[p] = kept ? Elem<BF16>::get(row[col[p]]) : 0.f;
+    }
+  }
+  // The teacher's probabilities p = softmax(t / T) over the kept entries: cols,
+  // probs, zs in LDS; returns 1 where there is any, else 0.  scratch: THREADS /
+  // 64 floats.
+  __device__ __forceinline__ float probabilities(const DistillArgs& a, int* cols, float* probs,
+                                                 float* zs, float* scratch, float k) {
+    constexpr int W = THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float m = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int e = p * THREADS + (int)threadIdx.x;
+      // a NaN that fmaxf drops comes back in the sum
+      if (e < a.K && col[p] >= 0) m = fmaxf(m, t[p]);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if (lane == 0) scratch[wave] = m;
+    __syncthreads();
+    for (int w = 0; w < W; ++w) m = fmaxf(m, scratch[w]);
+    __syncthreads();
+    float s = 0.f;
+    bool any = false;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int e = p * THREADS + (int)threadIdx.x;
+      if (e >= a.K) break;
+      t[p] = col[p] >= 0 ? exp2_hw((t[p] - m) * k) : 0.f;
+      s += t[p];
+      any |= col[p] >= 0;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
+    if (lane == 0) scratch[wave] = s;
+    const int some = __syncthreads_or(any);
+    s = 0.f;
+    for (int w = 0; w < W; ++w) s += scratch[w];
+    const float inv = 1.f / s;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int e = p * THREADS + (int)threadIdx.x;
+      if (e >= a.K) break;
+      cols[e] = col[p];
+      probs[e] = col[p] >= 0 ? t[p] * inv : 0.f;
+      zs[e] = z[p];
+    }
+    __syncthreads();
+    return some ? 1.f : 0.f;
+  }
+};
 
 // sum p (log p - log q) over the kept entries with p > 0, in every thread
-template <bool BF16, int THREADS>
-__device__ __forceinline__ float distill_loss(const DistillArgs& a, const int* cols,
-                                              const float* probs, float* scratch,
-                                              const typename Elem<BF16>::T* z, const RowStats& st,
+template <int THREADS>
+__device__ __forceinline__ float distill_loss(const DistillArgs& a, const float* probs,
+                                              const float* zs, float* scratch, const RowStats& st,
                                               float inv_t) {
   constexpr int W = THREADS / 64;
   float loss = 0.f;
   for (int e = threadIdx.x; e < a.K; e += THREADS) {
     const float p = probs[e];
     // p = 0 (too small for fp32, or no entry) adds 0; a NaN stays one
-    if (p != 0.f) loss += p * (logf(p) - row_logprob(st, Elem<BF16>::get(z[cols[e]]), inv_t));
+    if (p != 0.f) loss += p * (logf(p) - row_logprob(st, zs[e], inv_t));
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) loss += __shfl_xor(loss, o);
@@ -781,16 +827,19 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int par
   constexpr int W = THREADS / 64;
   __shared__ float red[3 * W];
   __shared__ int cols[kMaxTeacher];
-  __shared__ float probs[kMaxTeacher];
+  __shared__ float probs[kMaxTeacher], zs[kMaxTeacher];
   const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
   const long long items = (long long)a.r.N * parts;
   for (long long it = blockIdx.x; it < items; it += gridDim.x) {
     const int row = (int)(it / parts), part = (int)(it - (long long)row * parts);
     const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
+    Teacher<BF16, THREADS> teacher;
     float m, s;
+    if (!STATS || parts == 1) teacher.fetch(a, row);
     if constexpr (STATS) {
       Found<W> none{nullptr, nullptr, nullptr, 0};
       Run<false> run = part_stats<BF16, THREADS, U, false, false>(z, a.r.V, part, parts, k, none);
+      if (parts == 1) teacher.gather(a, z);
       run = run_block<THREADS>(run, k, red);
       m = run.m;
       s = run.s;
@@ -799,13 +848,14 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int par
         continue;
       }
     } else {
+      teacher.gather(a, z);
       m = a.stats[2LL * row];
       s = a.stats[2LL * row + 1];
     }
     const RowStats st = row_stats(m, s);
-    const float kept = teacher_probs<THREADS>(a, row, cols, probs, red, k);
+    const float kept = teacher.probabilities(a, cols, probs, zs, red, k);
     if constexpr (STATS) {
-      const float loss = distill_loss<BF16, THREADS>(a, cols, probs, red, z, st, inv_t);
+      const float loss = distill_loss<THREADS>(a, probs, zs, red, st, inv_t);
       if (threadIdx.x == 0) {
         a.loss[row] = loss;
         a.stats[2LL * row] = m;
@@ -821,10 +871,9 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int par
         probs[e] = g == 0.f ? 0.f : -g * probs[e];
         if (g == 0.f) cols[e] = -1;
       }
-      __syncthreads();
+      __syncthreads();  // (and the gathered logits are here: dz may be z)
       PointTerms<BF16, THREADS, kMaxTeacher, false> pt;
-      pt.take(cols, probs, a.K, z, a.r.V, part, parts, st.base, k, c0, 0.f);
-      __syncthreads();  // dz may be z
+      pt.take(cols, probs, zs, a.K, z, a.r.V, part, parts, st.base, k, c0, 0.f);
       part_grad<BF16, THREADS, U, false>(z, dz, a.r.V, part, parts, st.base, k, c0, 0.f);
       __syncthreads();
       pt.put(dz);
@@ -839,14 +888,17 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a, int pa
   using E = Elem<BF16>;
   __shared__ float red[4];
   __shared__ int cols[kMaxTeacher];
-  __shared__ float probs[kMaxTeacher];
+  __shared__ float probs[kMaxTeacher], zs[kMaxTeacher];
   const float inv_t = 1.f / a.r.temperature, k = kLog2e / a.r.temperature;
   const float* ws = static_cast<const float*>(a.workspace);
   for (int row = blockIdx.x; row < a.r.N; row += gridDim.x) {
     const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
     const int lane = threadIdx.x & 63;
+    Teacher<BF16, 256> teacher;
+    teacher.fetch(a, row);
     Run<false> run;
     if (lane < parts) run = run_load<false>(ws + 4 * ((long long)row * parts + lane));
+    teacher.gather(a, z);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       Run<false> b;
@@ -855,8 +907,8 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a, int pa
       run.join(b, k);
     }
     const RowStats st = row_stats(run.m, run.s);
-    teacher_probs<256>(a, row, cols, probs, red, k);
-    const float loss = distill_loss<BF16, 256>(a, cols, probs, red, z, st, inv_t);
+    teacher.probabilities(a, cols, probs, zs, red, k);
+    const float loss = distill_loss<256>(a, probs, zs, red, st, inv_t);
     if (threadIdx.x == 0) {
       a.loss[row] = loss;
       a.stats[2LL * row] = run.m;
