@@ -562,56 +562,69 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int pa
 }
 
 // ------------------------------------------------------------------ gradients
-// dz_j = e_j (c0 + c1 x_j), e_j = 2^{x_j}, over a part of a row.
-template <bool BF16, int THREADS, int U, bool LIN>
-__device__ __forceinline__ void part_grad(const typename Elem<BF16>::T* z,
-                                          typename Elem<BF16>::T* dz, int V, int part, int parts,
-                                          float base, float k, float c0, float c1) {
+// dz_j = e_j (c0 + c1 x_j), e_j = 2^{x_j}, over a part of a row.  The first round
+// of loads is made when the object is, ahead of what the gradient waits for.
+template <bool BF16, int THREADS, int U>
+struct PartGrad {
   using E = Elem<BF16>;
-  constexpr int VE = E::VE;
-  const Span sp = row_span<BF16>(z, V);
-  const int tid = threadIdx.x;
-  const int v0 = (int)((long long)sp.nvec * part / parts);
-  const int v1 = (int)((long long)sp.nvec * (part + 1) / parts);
-  const uint4* zv = reinterpret_cast<const uint4*>(z + sp.head);
-  uint4* dv = reinterpret_cast<uint4*>(dz + sp.head);
-  // rows of another alignment than their logits' are written element by element
-  const bool whole = ((reinterpret_cast<uintptr_t>(dv)) & 15) == 0;
-  // a row that adds nothing: exact zeros, whatever its logits are
-  const bool none = c0 == 0.f && c1 == 0.f;
-  auto grad = [&](float zj) {
-    const float x = (zj - base) * k;
-    const float e = exp2_hw(x);
-    return none ? 0.f : LIN ? e * fmaf(c1, fmaxf(x, kLowExp), c0) : e * c0;
-  };
-  for (int v = v0; v < v1; v += THREADS * U) {
-    uint4 u[U];
+  static constexpr int VE = E::VE;
+  const typename E::T* z;
+  Span sp;
+  int V, v0, v1;
+  bool first, last;  // the part has the row's head, tail
+  uint4 u[U];
+
+  __device__ __forceinline__ void load(int v) {
+    const uint4* zv = reinterpret_cast<const uint4*>(z + sp.head);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int at = v + i * THREADS + tid;
-      if (at < v1 && !none) u[i] = load_last(zv + at);
+      const int at = v + i * THREADS + (int)threadIdx.x;
+      if (at < v1) u[i] = load_last(zv + at);
     }
+  }
+  __device__ __forceinline__ PartGrad(const typename E::T* z_, int V_, int part, int parts)
+      : z(z_), sp(row_span<BF16>(z_, V_)), V(V_), first(part == 0), last(part == parts - 1) {
+    v0 = (int)((long long)sp.nvec * part / parts);
+    v1 = (int)((long long)sp.nvec * (part + 1) / parts);
+    load(v0);
+  }
+  template <bool LIN>
+  __device__ __forceinline__ void write(typename E::T* dz, float base, float k, float c0,
+                                        float c1) {
+    const int tid = threadIdx.x;
+    uint4* dv = reinterpret_cast<uint4*>(dz + sp.head);
+    // rows of another alignment than their logits' are written element by element
+    const bool whole = ((reinterpret_cast<uintptr_t>(dv)) & 15) == 0;
+    // a row that adds nothing: exact zeros, whatever its logits are
+    const bool none = c0 == 0.f && c1 == 0.f;
+    auto grad = [&](float zj) {
+      const float x = (zj - base) * k;
+      const float e = exp2_hw(x);
+      return none ? 0.f : LIN ? e * fmaf(c1, fmaxf(x, kLowExp), c0) : e * c0;
+    };
+    for (int v = v0; v < v1; v += THREADS * U) {
+      if (v > v0 && !none) load(v);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int at = v + i * THREADS + tid;
-      if (at < v1) {
-        float f[VE];
-        E::unpack(u[i], f);
+      for (int i = 0; i < U; ++i) {
+        const int at = v + i * THREADS + tid;
+        if (at < v1) {
+          float f[VE];
+          E::unpack(u[i], f);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) f[j] = grad(f[j]);
-        if (whole) {
-          store_last(dv + at, E::pack(f));
-        } else {
+          for (int j = 0; j < VE; ++j) f[j] = grad(f[j]);
+          if (whole) {
+            store_last(dv + at, E::pack(f));
+          } else {
 #pragma unroll
-          for (int j = 0; j < VE; ++j) dz[sp.head + at * VE + j] = E::put(f[j]);
+            for (int j = 0; j < VE; ++j) dz[sp.head + at * VE + j] = E::put(f[j]);
+          }
         }
       }
     }
+    if (first && tid < sp.head) dz[tid] = E::put(grad(E::get(z[tid])));
+    if (last && tid < V - sp.tail) dz[sp.tail + tid] = E::put(grad(E::get(z[sp.tail + tid])));
   }
-  if (part == 0 && tid < sp.head) dz[tid] = E::put(grad(E::get(z[tid])));
-  if (part == parts - 1 && tid < V - sp.tail)
-    dz[sp.tail + tid] = E::put(grad(E::get(z[sp.tail + tid])));
-}
+};
 
 // Whether column col lies in this part of the row.
 template <bool BF16>
@@ -687,6 +700,7 @@ __global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LogprobGradArgs a
     auto* dz = static_cast<typename E::T*>(a.dz) + (long long)row * a.ldd;
     const float s = a.stats[2LL * row + 1];
     const RowStats st = row_stats(a.stats[2LL * row], s);
+    PartGrad<BF16, THREADS, U> pg(z, a.r.V, part, parts);
     for (int e = threadIdx.x; e < n; e += THREADS) {
       const int64_t c = e == 0 ? (a.dlogprob ? a.tokens[row] : -1)
                                : a.top_ids[(long long)row * a.top + e - 1];
@@ -706,9 +720,9 @@ __global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LogprobGradArgs a
     pt.take(cols, wts, nullptr, n, z, a.r.V, part, parts, st.base, k, c0, c1);
     __syncthreads();  // dz may be z
     if (c1 == 0.f)
-      part_grad<BF16, THREADS, U, false>(z, dz, a.r.V, part, parts, st.base, k, c0, 0.f);
+      pg.template write<false>(dz, st.base, k, c0, 0.f);
     else
-      part_grad<BF16, THREADS, U, true>(z, dz, a.r.V, part, parts, st.base, k, c0, c1);
+      pg.template write<true>(dz, st.base, k, c0, c1);
     __syncthreads();
     pt.put(dz);
     __syncthreads();
@@ -822,7 +836,7 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, const float*
 // is written.  parts > 1 with STATS: only the part's statistics are, into the
 // workspace.
 template <bool BF16, int THREADS, int U, bool STATS, bool GRAD>
-__global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int parts) {
+__global__ __launch_bounds__(THREADS, 6) void distill_kernel(DistillArgs a, int parts) {
   using E = Elem<BF16>;
   constexpr int W = THREADS / 64;
   __shared__ float red[3 * W];
@@ -853,6 +867,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int par
       s = a.stats[2LL * row + 1];
     }
     const RowStats st = row_stats(m, s);
+    PartGrad<BF16, THREADS, GRAD ? U : 1> pg(z, GRAD ? a.r.V : 0, part, parts);
     const float kept = teacher.probabilities(a, cols, probs, zs, red, k);
     if constexpr (STATS) {
       const float loss = distill_loss<THREADS>(a, probs, zs, red, st, inv_t);
@@ -874,7 +889,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int par
       __syncthreads();  // (and the gathered logits are here: dz may be z)
       PointTerms<BF16, THREADS, kMaxTeacher, false> pt;
       pt.take(cols, probs, zs, a.K, z, a.r.V, part, parts, st.base, k, c0, 0.f);
-      part_grad<BF16, THREADS, U, false>(z, dz, a.r.V, part, parts, st.base, k, c0, 0.f);
+      pg.template write<false>(dz, st.base, k, c0, 0.f);
       __syncthreads();
       pt.put(dz);
     }
@@ -919,6 +934,7 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a, int pa
 }
 
 constexpr int kThreads = 512;
+constexpr int kFewThreads = 256;
 constexpr int kUnroll = 4;
 
 // Parts a row is cut into: with fewer rows than CUs some would have nothing to
@@ -930,14 +946,27 @@ int row_parts(int N, int V, bool bf16, bool top = false) {
   const int p = want < most ? want : most;
   return p < 1 ? 1 : p > kMaxParts ? kMaxParts : p;
 }
+// Short rows that are not cut go to workgroups of 256 threads: what they wait for
+// between loading and writing a row is a larger part then, and more rows at a
+// time cover it.  16384 x 8192 bf16: forward 146 -> 72 us, gradient 161 -> 141;
+// 8192 x 32000 bf16: forward 111 -> 98, gradient 205 -> 237 us.
+bool short_rows(int V, bool bf16, int parts, bool grad_only) {
+  return parts == 1 && V / (bf16 ? 8 : 4) <= (grad_only ? 2048 : 4096);
+}
+
 dim3 grid_of(long long items) { return dim3((unsigned)(items < kMaxGrid ? items : kMaxGrid)); }
 
 template <bool BF16, bool TOP>
 hipError_t logprob_run(const LogprobArgs& a, hipStream_t st) {
   const int parts = row_parts(a.r.N, a.r.V, BF16, TOP);
+  const dim3 grid = grid_of((long long)a.r.N * parts);
   timing_before("logprobs", st);
-  hipLaunchKernelGGL((logprob_kernel<BF16, kThreads, kUnroll, TOP>),
-                     grid_of((long long)a.r.N * parts), dim3(kThreads), 0, st, a, parts);
+  if (short_rows(a.r.V, BF16, parts, false))
+    hipLaunchKernelGGL((logprob_kernel<BF16, kFewThreads, kUnroll, TOP>), grid, dim3(kFewThreads),
+                       0, st, a, parts);
+  else
+    hipLaunchKernelGGL((logprob_kernel<BF16, kThreads, kUnroll, TOP>), grid, dim3(kThreads), 0, st,
+                       a, parts);
   timing_after(st);
   if (hipError_t e = hipGetLastError()) return e;
   if (parts == 1) return hipSuccess;
@@ -949,31 +978,47 @@ hipError_t logprob_run(const LogprobArgs& a, hipStream_t st) {
 }
 
 template <bool BF16>
+hipError_t logprob_grad_run(const LogprobGradArgs& a, hipStream_t st) {
+  const int parts = row_parts(a.r.N, a.r.V, BF16);
+  const dim3 grid = grid_of((long long)a.r.N * parts);
+  timing_before("logprobs_grad", st);
+  if (short_rows(a.r.V, BF16, parts, true))
+    hipLaunchKernelGGL((logprob_grad_kernel<BF16, kFewThreads, kUnroll>), grid, dim3(kFewThreads),
+                       0, st, a, parts);
+  else
+    hipLaunchKernelGGL((logprob_grad_kernel<BF16, kThreads, kUnroll>), grid, dim3(kThreads), 0, st,
+                       a, parts);
+  timing_after(st);
+  return hipGetLastError();
+}
+
+template <bool BF16, bool STATS, bool GRAD>
+hipError_t distill_part(const DistillArgs& a, int parts, const char* label, hipStream_t st) {
+  const dim3 grid = grid_of((long long)a.r.N * parts);
+  timing_before(label, st);
+  if (short_rows(a.r.V, BF16, parts, !STATS))
+    hipLaunchKernelGGL((distill_kernel<BF16, kFewThreads, kUnroll, STATS, GRAD>), grid,
+                       dim3(kFewThreads), 0, st, a, parts);
+  else
+    hipLaunchKernelGGL((distill_kernel<BF16, kThreads, kUnroll, STATS, GRAD>), grid,
+                       dim3(kThreads), 0, st, a, parts);
+  timing_after(st);
+  return hipGetLastError();
+}
+
+template <bool BF16>
 hipError_t distill_run(const DistillArgs& a, hipStream_t st) {
   const int parts = row_parts(a.r.N, a.r.V, BF16);
-  const dim3 blk(kThreads);
   if (a.loss) {
-    timing_before("distill", st);
-    if (a.dz && parts == 1)
-      hipLaunchKernelGGL((distill_kernel<BF16, kThreads, kUnroll, true, true>), grid_of(a.r.N),
-                         blk, 0, st, a, 1);
-    else
-      hipLaunchKernelGGL((distill_kernel<BF16, kThreads, kUnroll, true, false>),
-                         grid_of((long long)a.r.N * parts), blk, 0, st, a, parts);
-    timing_after(st);
-    if (hipError_t e = hipGetLastError()) return e;
+    if (a.dz && parts == 1) return distill_part<BF16, true, true>(a, 1, "distill", st);
+    if (hipError_t e = distill_part<BF16, true, false>(a, parts, "distill", st)) return e;
     if (parts == 1) return hipSuccess;
     timing_before("distill_join", st);
     hipLaunchKernelGGL((distill_join_kernel<BF16>), grid_of(a.r.N), dim3(256), 0, st, a, parts);
     timing_after(st);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  if (!a.dz) return hipSuccess;
-  timing_before("distill_grad", st);
-  hipLaunchKernelGGL((distill_kernel<BF16, kThreads, kUnroll, false, true>),
-                     grid_of((long long)a.r.N * parts), blk, 0, st, a, parts);
-  timing_after(st);
-  return hipGetLastError();
+  return a.dz ? distill_part<BF16, false, true>(a, parts, "distill_grad", st) : hipSuccess;
 }
 
 }  // namespace
@@ -990,17 +1035,7 @@ hipError_t logprob_launch(const LogprobArgs& a, hipStream_t stream) {
 }
 
 hipError_t logprob_grad_launch(const LogprobGradArgs& a, hipStream_t stream) {
-  const int parts = row_parts(a.r.N, a.r.V, a.r.bf16 != 0);
-  const dim3 grid = grid_of((long long)a.r.N * parts);
-  timing_before("logprobs_grad", stream);
-  if (a.r.bf16)
-    hipLaunchKernelGGL((logprob_grad_kernel<true, kThreads, kUnroll>), grid, dim3(kThreads), 0,
-                       stream, a, parts);
-  else
-    hipLaunchKernelGGL((logprob_grad_kernel<false, kThreads, kUnroll>), grid, dim3(kThreads), 0,
-                       stream, a, parts);
-  timing_after(stream);
-  return hipGetLastError();
+  return a.r.bf16 ? logprob_grad_run<true>(a, stream) : logprob_grad_run<false>(a, stream);
 }
 
 size_t distill_workspace_bytes(int N, int V, int bf16) {
