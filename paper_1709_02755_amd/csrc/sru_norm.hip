@@ -13,6 +13,7 @@
 namespace sru {
 namespace {
 
+typedef unsigned Quad __attribute__((ext_vector_type(4)));
 template <bool BF16>
 struct Mem {
   using T = float;
@@ -49,7 +50,8 @@ __device__ __forceinline__ void load(const typename Mem<BF16>::T* p, float* f) {
     }
   }
 }
-template <bool BF16, int VE>
+// LAST: past the caches, for what is not read again soon.
+template <bool BF16, int VE, bool LAST = false>
 __device__ __forceinline__ void store(typename Mem<BF16>::T* p, const float* f) {
   if constexpr (VE == 1) {
     if constexpr (BF16) *p = __builtin_bit_cast(uint16_t, (__bf16)f[0]);
@@ -60,25 +62,84 @@ __device__ __forceinline__ void store(typename Mem<BF16>::T* p, const float* f) 
     for (int i = 0; i < 4; ++i)
       w[i] = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)f[2 * i]) |
              ((unsigned)__builtin_bit_cast(uint16_t, (__bf16)f[2 * i + 1]) << 16);
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    const Quad q = {w[0], w[1], w[2], w[3]};
+    if constexpr (LAST) __builtin_nontemporal_store(q, reinterpret_cast<Quad*>(p));
+    else *reinterpret_cast<Quad*>(p) = q;
   } else {
 #pragma unroll
-    for (int i = 0; i < VE; i += 4)
-      *reinterpret_cast<float4*>(p + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+    for (int i = 0; i < VE; i += 4) {
+      const Quad q = {__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]),
+                      __float_as_uint(f[i + 3])};
+      if constexpr (LAST) __builtin_nontemporal_store(q, reinterpret_cast<Quad*>(p + i));
+      else *reinterpret_cast<Quad*>(p + i) = q;
+    }
   }
 }
 
-// How a kernel holds a row: NW waves, each thread C chunks of VE consecutive
-// columns, the chunks of a row dealt to its threads in turn.  With one wave to
-// a row a workgroup works on four rows at a time.
-template <int VE_, int C_, int NW_>
+// How a kernel holds a row: LANES threads, each C chunks of VE consecutive
+// columns, the chunks of a row dealt to its threads in turn.  Rows of up to a
+// wave (16, 32 or 64 lanes) come 256 / LANES to a workgroup; their sums need no
+// barrier.
+template <int VE_, int C_, int LANES_>
 struct Hold {
-  static constexpr int VE = VE_, C = C_, NW = NW_, F = VE_ * C_;
-  static constexpr int ROWS = NW_ == 1 ? 4 : 1;
-  static constexpr int THREADS = 64 * NW_ * ROWS;
-  __device__ static int lane() { return NW == 1 ? threadIdx.x & 63 : threadIdx.x; }
-  __device__ static int sub() { return NW == 1 ? threadIdx.x >> 6 : 0; }
-  __device__ static int col(int c) { return (c * NW * 64 + lane()) * VE; }
+  static constexpr int VE = VE_, C = C_, LANES = LANES_, F = VE_ * C_;
+  static constexpr int NW = LANES_ <= 64 ? 1 : LANES_ / 64;  // waves of a row
+  static constexpr int ROWS = NW == 1 ? 256 / LANES_ : 1;
+  static constexpr int THREADS = LANES_ * ROWS;
+  __device__ static int lane() { return NW == 1 ? threadIdx.x % LANES : threadIdx.x; }
+  __device__ static int sub() { return NW == 1 ? threadIdx.x / LANES : 0; }
+  __device__ static int col(int c) { return (c * LANES + lane()) * VE; }
+};
+
+// F columns of a row as they lie in memory; columns past d are 0.
+template <class H, bool BF16>
+struct Raw {
+  static constexpr int Q = H::VE * (BF16 ? 2 : 4) / 16;  // 16-byte pieces of a chunk
+  uint4 q[Q ? H::C * Q : 1];
+  typename Mem<BF16>::T e[Q ? 1 : H::C];
+  __device__ __forceinline__ void load(const void* p, long long off, int d) {
+    const auto* at = static_cast<const typename Mem<BF16>::T*>(p) + off;
+#pragma unroll
+    for (int c = 0; c < H::C; ++c) {
+      const int col = H::col(c);
+      if constexpr (Q > 0) {
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+          q[c * Q + i] = make_uint4(0, 0, 0, 0);
+          if (col < d) q[c * Q + i] = reinterpret_cast<const uint4*>(at + col)[i];
+        }
+      } else {
+        e[c] = 0;
+        if (col < d) e[c] = at[col];
+      }
+    }
+  }
+  __device__ __forceinline__ void get(float (&f)[H::F]) const {
+#pragma unroll
+    for (int c = 0; c < H::C; ++c) {
+      if constexpr (Q > 0 && BF16) {
+        const unsigned w[4] = {q[c].x, q[c].y, q[c].z, q[c].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f[c * H::VE + 2 * i] = __uint_as_float(w[i] << 16);
+          f[c * H::VE + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+      } else if constexpr (Q > 0) {
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+          const uint4& u = q[c * Q + i];
+          f[c * H::VE + 4 * i] = __uint_as_float(u.x);
+          f[c * H::VE + 4 * i + 1] = __uint_as_float(u.y);
+          f[c * H::VE + 4 * i + 2] = __uint_as_float(u.z);
+          f[c * H::VE + 4 * i + 3] = __uint_as_float(u.w);
+        }
+      } else if constexpr (BF16) {
+        f[c] = __uint_as_float((unsigned)e[c] << 16);
+      } else {
+        f[c] = e[c];
+      }
+    }
+  }
 };
 
 // F columns of a row; columns past d are 0.
@@ -96,14 +157,14 @@ __device__ __forceinline__ void load_row(const void* p, long long off, int d, fl
     }
   }
 }
-template <class H, bool BF16>
+template <class H, bool BF16, bool LAST = false>
 __device__ __forceinline__ void store_row(const void* p, long long off, int d,
                                           const float (&f)[H::F]) {
   auto* q = static_cast<typename Mem<BF16>::T*>(const_cast<void*>(p)) + off;
 #pragma unroll
   for (int c = 0; c < H::C; ++c) {
     const int col = H::col(c);
-    if (col < d) store<BF16, H::VE>(q + col, f + c * H::VE);
+    if (col < d) store<BF16, H::VE, LAST>(q + col, f + c * H::VE);
   }
 }
 
@@ -111,7 +172,7 @@ __device__ __forceinline__ void store_row(const void* p, long long off, int d,
 template <class H>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+  for (int o = 1; o < (H::LANES < 64 ? H::LANES : 64); o <<= 1) v += __shfl_xor(v, o);
   if constexpr (H::NW > 1) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -134,7 +195,7 @@ __global__ __launch_bounds__(H::THREADS) void norm_kernel(NormArgs a) {
   for (long long m0 = (long long)blockIdx.x * H::ROWS; m0 < a.M;
        m0 += (long long)gridDim.x * H::ROWS) {
     const long long m = m0 + H::sub();
-    if (H::NW == 1 && m >= a.M) break;  // a wave's own row: it meets no barrier
+    if (H::NW == 1 && m >= a.M) break;  // the threads of a row meet no barrier
     float x[H::F], rx = 0.f, ry = 0.f;
     load_row<H, RBF>(a.x.p, m * a.x.ld, d, x);
     if (a.y.p) {
@@ -160,7 +221,8 @@ __global__ __launch_bounds__(H::THREADS) void norm_kernel(NormArgs a) {
       if (a.scale) load_row<H, false>(a.scale, 0, d, w);
 #pragma unroll
       for (int j = 0; j < H::F; ++j) x[j] = a.scale ? fmaf(w[j], y[j], x[j]) : x[j] + y[j];
-      store_row<H, RBF>(a.x_out.p, m * a.x_out.ld, d, x);
+      // next read a block later (16384 x 1024 bf16 beside fp32 56 -> 51 us)
+      store_row<H, RBF, true>(a.x_out.p, m * a.x_out.ld, d, x);
     }
     if (a.w_pre) {
       float w[H::F];
@@ -186,25 +248,60 @@ __global__ __launch_bounds__(H::THREADS) void norm_kernel(NormArgs a) {
 // Every workgroup adds its rows' terms of the three parameter gradients in
 // registers and leaves one row of sums, [workgroup, 3, d].
 template <class H, bool ABF, bool RBF>
+struct GradRow {
+  Raw<H, RBF> x, dx;
+  Raw<H, ABF> y, z, go;
+  __device__ __forceinline__ void load(const NormArgs& a, long long m) {
+    if (m >= a.M) return;
+    x.load(a.x.p, m * a.x.ld, a.d);
+    if (a.y.p) y.load(a.y.p, m * a.y.ld, a.d);
+    if (a.z.p) z.load(a.z.p, m * a.z.ld, a.d);
+    if (a.go.p) go.load(a.go.p, m * a.go.ld, a.d);
+    if (a.dx_out.p) dx.load(a.dx_out.p, m * a.dx_out.ld, a.d);
+  }
+};
+
+// When a row's tensors are loaded.  Rows of up to a wave: all at once, in front
+// (2 or 3 waves run on a SIMD then, fewer than with loads where they are used,
+// but with more in flight: 16384 x 1024 bf16 beside fp32 104 -> 89 us, 65536 x
+// 256 145 -> 85).  256 threads to a row, which wait for each other twice a row:
+// while the row before is worked on (8192 x 2048 121 -> 97 us).  Wider rows: each
+// where it is used (4096 x 4096 98 us, 105 in front).
+template <class H, bool ABF, bool RBF>
 __global__ __launch_bounds__(H::THREADS) void norm_grad_kernel(NormArgs a) {
+  constexpr bool AHEAD = H::LANES == 256, WHOLE = AHEAD || H::NW == 1;
   __shared__ float lds[H::NW];
-  __shared__ float sums[H::ROWS > 1 ? H::ROWS * 64 * H::F : 1];
+  __shared__ float sums[H::ROWS > 1 ? H::THREADS * H::F : 1];
   const int d = a.d;
   float gw_post[H::F], gscale[H::F], gw_pre[H::F];
 #pragma unroll
   for (int j = 0; j < H::F; ++j) gw_post[j] = gscale[j] = gw_pre[j] = 0.f;
 
-  for (long long m0 = (long long)blockIdx.x * H::ROWS; m0 < a.M;
-       m0 += (long long)gridDim.x * H::ROWS) {
+  const long long step = (long long)gridDim.x * H::ROWS;
+  GradRow<H, ABF, RBF> row, next;
+  if constexpr (AHEAD) next.load(a, (long long)blockIdx.x * H::ROWS + H::sub());
+  for (long long m0 = (long long)blockIdx.x * H::ROWS; m0 < a.M; m0 += step) {
     const long long m = m0 + H::sub();
     if (H::NW == 1 && m >= a.M) break;
+    if constexpr (AHEAD) {
+      row = next;
+      next.load(a, m + step);
+    } else if constexpr (WHOLE) {
+      row.load(a, m);
+    }
     float x[H::F], y[H::F], z[H::F], u[H::F], dx[H::F], w[H::F];
-    load_row<H, RBF>(a.x.p, m * a.x.ld, d, x);
-    if (a.y.p) load_row<H, ABF>(a.y.p, m * a.y.ld, d, y);
-    if (a.z.p) load_row<H, ABF>(a.z.p, m * a.z.ld, d, z);
-    if (a.dx_out.p) {
-      load_row<H, RBF>(a.dx_out.p, m * a.dx_out.ld, d, dx);
+    if constexpr (WHOLE) {
+      row.x.get(x);
+      if (a.y.p) row.y.get(y);
+      if (a.z.p) row.z.get(z);
+      if (a.dx_out.p) row.dx.get(dx);
     } else {
+      load_row<H, RBF>(a.x.p, m * a.x.ld, d, x);
+      if (a.y.p) load_row<H, ABF>(a.y.p, m * a.y.ld, d, y);
+      if (a.z.p) load_row<H, ABF>(a.z.p, m * a.z.ld, d, z);
+      if (a.dx_out.p) load_row<H, RBF>(a.dx_out.p, m * a.dx_out.ld, d, dx);
+    }
+    if (!a.dx_out.p) {
 #pragma unroll
       for (int j = 0; j < H::F; ++j) dx[j] = 0.f;
     }
@@ -232,7 +329,8 @@ __global__ __launch_bounds__(H::THREADS) void norm_grad_kernel(NormArgs a) {
     if (a.w_pre && a.go.p) {
       const float rx = a.rstd[2 * m + 1];
       float t[H::F];
-      load_row<H, ABF>(a.go.p, m * a.go.ld, d, t);
+      if constexpr (WHOLE) row.go.get(t);
+      else load_row<H, ABF>(a.go.p, m * a.go.ld, d, t);
       load_row<H, false>(a.w_pre, 0, d, w);
       float s = 0.f;
 #pragma unroll
@@ -246,7 +344,7 @@ __global__ __launch_bounds__(H::THREADS) void norm_grad_kernel(NormArgs a) {
 #pragma unroll
       for (int j = 0; j < H::F; ++j) dx[j] += rx * (t[j] - x[j] * s);
     }
-    store_row<H, RBF>(a.dx.p, m * a.dx.ld, d, dx);
+    store_row<H, RBF, true>(a.dx.p, m * a.dx.ld, d, dx);
     if (!a.y.p) continue;
 #pragma unroll
     for (int j = 0; j < H::F; ++j) gscale[j] = fmaf(dx[j], u[j], gscale[j]);
@@ -295,14 +393,14 @@ __global__ __launch_bounds__(H::THREADS) void norm_grad_kernel(NormArgs a) {
     if constexpr (H::ROWS > 1) {
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < H::F; ++j) sums[(H::sub() * H::F + j) * 64 + H::lane()] = g[j];
+      for (int j = 0; j < H::F; ++j) sums[(H::sub() * H::F + j) * H::LANES + H::lane()] = g[j];
       __syncthreads();
       if (H::sub() != 0) return;
 #pragma unroll
       for (int j = 0; j < H::F; ++j) {
         float s = g[j];
 #pragma unroll
-        for (int r = 1; r < H::ROWS; ++r) s += sums[(r * H::F + j) * 64 + H::lane()];
+        for (int r = 1; r < H::ROWS; ++r) s += sums[(r * H::F + j) * H::LANES + H::lane()];
         g[j] = s;
       }
     }
@@ -338,18 +436,19 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(NormArgs a, int rows) {
   }
 }
 
-// Workgroups of the gradient: each leaves one row of sums, so only about as
-// many as run at a time.
+// Workgroups of the gradient: each leaves one row of sums, so only as many as
+// run at a time (by the registers they take).
+int rows_at_once(int d) { return d <= 128 ? 16 : d <= 256 ? 8 : d <= 1024 ? 4 : 1; }
 int grad_blocks(int M, int d) {
-  const int rows = d <= 1024 ? 4 : 1;  // rows a workgroup has at a time
-  const int most = d <= 1024 ? 512 : d <= 2048 ? 512 : d <= 4096 ? 512 : 256;
-  const int want = (M + rows - 1) / rows;
+  const int most = d <= 512 ? 768 : d <= 4096 ? 512 : 256;
+  const int want = (int)(((long long)M + rows_at_once(d) - 1) / rows_at_once(d));
   return want < most ? want : most;
 }
 
 template <class H, bool ABF, bool RBF>
 hipError_t launch(const NormArgs& a, bool grad, hipStream_t st) {
   if (grad) {
+    static_assert(H::F == 8 || H::F == 16, "columns of a thread");
     const int blocks = grad_blocks(a.M, a.d);
     timing_before("norm_grad", st);
     hipLaunchKernelGGL((norm_grad_kernel<H, ABF, RBF>), dim3(blocks), dim3(H::THREADS), 0, st, a);
@@ -371,17 +470,19 @@ hipError_t launch(const NormArgs& a, bool grad, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Waves and columns a thread by the width: a row's columns stay in registers,
-// 8 to a thread (16 up to 1024 columns, where one wave then holds a row and
-// needs no barrier, and past 8192).
+// Threads a row and columns a thread by the width: a row's columns stay in
+// registers, 8 to a thread (16 up to 1024 columns, where one wave then holds a
+// row and needs no barrier, and past 8192).
 template <int VE, bool ABF, bool RBF>
 hipError_t by_width(const NormArgs& a, bool grad, hipStream_t st) {
-  if (a.d <= 512) return launch<Hold<VE, 8 / VE, 1>, ABF, RBF>(a, grad, st);
-  if (a.d <= 1024) return launch<Hold<VE, 16 / VE, 1>, ABF, RBF>(a, grad, st);
-  if (a.d <= 2048) return launch<Hold<VE, 8 / VE, 4>, ABF, RBF>(a, grad, st);
-  if (a.d <= 4096) return launch<Hold<VE, 8 / VE, 8>, ABF, RBF>(a, grad, st);
-  if (a.d <= 8192) return launch<Hold<VE, 8 / VE, 16>, ABF, RBF>(a, grad, st);
-  return launch<Hold<VE, 16 / VE, 16>, ABF, RBF>(a, grad, st);
+  if (a.d <= 128) return launch<Hold<VE, 8 / VE, 16>, ABF, RBF>(a, grad, st);
+  if (a.d <= 256) return launch<Hold<VE, 8 / VE, 32>, ABF, RBF>(a, grad, st);
+  if (a.d <= 512) return launch<Hold<VE, 8 / VE, 64>, ABF, RBF>(a, grad, st);
+  if (a.d <= 1024) return launch<Hold<VE, 16 / VE, 64>, ABF, RBF>(a, grad, st);
+  if (a.d <= 2048) return launch<Hold<VE, 8 / VE, 256>, ABF, RBF>(a, grad, st);
+  if (a.d <= 4096) return launch<Hold<VE, 8 / VE, 512>, ABF, RBF>(a, grad, st);
+  if (a.d <= 8192) return launch<Hold<VE, 8 / VE, 1024>, ABF, RBF>(a, grad, st);
+  return launch<Hold<VE, 16 / VE, 1024>, ABF, RBF>(a, grad, st);
 }
 
 // 16-byte accesses need every row of every tensor to start on 16 bytes.
