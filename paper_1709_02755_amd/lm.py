@@ -62,12 +62,14 @@ def _pitch(t, name, shape, dtype, device):
     return ld
 
 
-def _out(out, name, shape, dtype, device):
-    """out[name] if the caller gave it (checked), else a new tensor."""
+def _out(out, name, shape, dtype, like):
+    """out[name] if the caller gave it (checked), else a new tensor on the
+    device of `like` (whose method makes it at half the cost of torch.empty: a
+    small call is bound by the host)."""
     t = None if out is None else out.get(name)
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    _req(t, name, shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+    _req(t, name, shape, dtype=dtype, device=like.device)
     return t
 
 
@@ -86,7 +88,7 @@ def _logits(logits, temperature):
 def _dlogits(dlogits, logits, dv):
     """(dlogits, its pitch): the caller's, which may be the logits, or new."""
     if dlogits is None:
-        dlogits = torch.empty(tuple(logits.shape), dtype=logits.dtype, device=dv)
+        dlogits = logits.new_empty(logits.shape)
     return dlogits, _pitch(dlogits, "dlogits", logits.shape, logits.dtype, dv)
 
 
@@ -103,11 +105,11 @@ def token_logprobs(logits, tokens, top=0, temperature=1.0, out=None, ws=None):
     be strided; logits of -inf are tokens that are not possible."""
     code, N, V, dv, ld = _logits(logits, temperature)
     _req(tokens, "tokens", (N,), dtype=_I64, device=dv)
-    o = dict(logprob=_out(out, "logprob", (N,), _F32, dv),
-             entropy=_out(out, "entropy", (N,), _F32, dv),
-             stats=_out(out, "stats", (N, 2), _F32, dv),
-             top_ids=_out(out, "top_ids", (N, top), _I64, dv) if top else None,
-             top_logprobs=_out(out, "top_logprobs", (N, top), _F32, dv) if top else None)
+    o = dict(logprob=_out(out, "logprob", (N,), _F32, logits),
+             entropy=_out(out, "entropy", (N,), _F32, logits),
+             stats=_out(out, "stats", (N, 2), _F32, logits),
+             top_ids=_out(out, "top_ids", (N, top), _I64, logits) if top else None,
+             top_logprobs=_out(out, "top_logprobs", (N, top), _F32, logits) if top else None)
     lib = sru.lib()
     ws, nbytes = _ws(ws, lib.sru_token_logprobs_workspace_bytes(N, V, code, top), dv)
     st = lib.sru_token_logprobs(_ptr(logits), ld, code, _ptr(tokens), N, V, top, temperature,
@@ -171,7 +173,7 @@ def distill_forward(logits, teacher_ids, teacher_logits, temperature=1.0, out=No
     normalised among themselves.  A row without any has loss 0."""
     code, N, V, dv, ld = _logits(logits, temperature)
     tcode, K = _teacher(teacher_ids, teacher_logits, N, dv)
-    o = dict(loss=_out(out, "loss", (N,), _F32, dv), stats=_out(out, "stats", (N, 2), _F32, dv))
+    o = dict(loss=_out(out, "loss", (N,), _F32, logits), stats=_out(out, "stats", (N, 2), _F32, logits))
     lib = sru.lib()
     ws, nbytes = _ws(ws, lib.sru_distill_workspace_bytes(N, V, code), dv)
     st = lib.sru_distill_forward(_ptr(logits), ld, code, _ptr(teacher_ids), _ptr(teacher_logits),
@@ -205,7 +207,7 @@ def distill_forward_backward(logits, teacher_ids, teacher_logits, dloss, tempera
     code, N, V, dv, ld = _logits(logits, temperature)
     tcode, K = _teacher(teacher_ids, teacher_logits, N, dv)
     _req(dloss, "dloss", (N,), device=dv)
-    o = dict(loss=_out(out, "loss", (N,), _F32, dv), stats=_out(out, "stats", (N, 2), _F32, dv))
+    o = dict(loss=_out(out, "loss", (N,), _F32, logits), stats=_out(out, "stats", (N, 2), _F32, logits))
     o["dlogits"], ldd = _dlogits(dlogits, logits, dv)
     lib = sru.lib()
     ws, nbytes = _ws(ws, lib.sru_distill_workspace_bytes(N, V, code), dv)
@@ -273,12 +275,13 @@ def _norm_inputs(x, y, z, w_post, scale, w_pre):
     return x.numel() // d if d else 0, d, act, code, res, dv, pitch
 
 
-def _row_out(out, name, shape, dtype, device):
-    """(out[name] or a new tensor, its row pitch)."""
+def _row_out(out, name, like):
+    """(out[name] or a new tensor, of the shape and type of `like`; its row
+    pitch)."""
     t = None if out is None else out.get(name)
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device), shape[-1]
-    return t, _row_pitch(t, name, shape, dtype, device)
+        return like.new_empty(like.shape), like.shape[-1]
+    return t, _row_pitch(t, name, like.shape, like.dtype, like.device)
 
 
 def residual_norm_forward(x, y=None, w_post=None, z=None, scale=None, w_pre=None,
@@ -297,10 +300,10 @@ def residual_norm_forward(x, y=None, w_post=None, z=None, scale=None, w_pre=None
     M, d, act, code, res, dv, (ldx, ldy, ldz) = _norm_inputs(x, y, z, w_post, scale, w_pre)
     x_out, o, ldxo, ldo = None, None, 0, 0
     if y is not None:
-        x_out, ldxo = _row_out(out, "x_out", x.shape, x.dtype, dv)
+        x_out, ldxo = _row_out(out, "x_out", x)
     if w_pre is not None:
-        o, ldo = _row_out(out, "o", x.shape, act, dv)
-    rstd = _out(out, "rstd", tuple(x.shape[:-1]) + (2,), _F32, dv)
+        o, ldo = _row_out(out, "o", x if y is None else y)
+    rstd = _out(out, "rstd", x.shape[:-1] + (2,), _F32, x)
     st = sru.lib().sru_residual_norm_forward(M, d, code, res, gate, eps, _ptr(x), ldx, _ptr(y),
                                              ldy, _ptr(z), ldz, _ptr(w_post), _ptr(scale),
                                              _ptr(w_pre), _ptr(x_out), ldxo, _ptr(o), ldo,
@@ -321,11 +324,11 @@ def residual_norm_backward(x, y, rstd, dx_out=None, do=None, w_post=None, z=None
     lddxo = _row_pitch(dx_out, "dx_out", shape, x.dtype, dv)
     lddo = _row_pitch(do, "do", shape, act, dv)
     g = {}
-    g["dx"], lddx = _row_out(out, "dx", shape, x.dtype, dv)
-    g["dy"], lddy = _row_out(out, "dy", shape, act, dv) if y is not None else (None, 0)
-    g["dz"], lddz = _row_out(out, "dz", shape, act, dv) if z is not None else (None, 0)
+    g["dx"], lddx = _row_out(out, "dx", x)
+    g["dy"], lddy = _row_out(out, "dy", y) if y is not None else (None, 0)
+    g["dz"], lddz = _row_out(out, "dz", z) if z is not None else (None, 0)
     for n, w in (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre)):
-        g[n] = None if w is None else _out(out, n, (d,), _F32, dv)
+        g[n] = None if w is None else _out(out, n, (d,), _F32, x)
     lib = sru.lib()
     ws, nbytes = _ws(ws, lib.sru_residual_norm_backward_workspace_bytes(M, d), dv)
     st = lib.sru_residual_norm_backward(
@@ -372,12 +375,14 @@ def _lru_inputs(x, r, i, lam, mask, reset):
     return shape, code, dv, steps
 
 
-def _seq_out(out, name, shape, dtype, device):
-    """(out[name] or a new tensor, its distances)."""
+def _seq_out(out, name, like):
+    """(out[name] or a new tensor, of the shape and type of `like`; its
+    distances)."""
     t = None if out is None else out.get(name)
     if t is None:
-        t = torch.empty(shape, dtype=dtype, device=device)
-    return t, _seq(t, name, shape, dtype, device)
+        _, B, d = like.shape
+        return like.new_empty(like.shape), (B * d, d)
+    return t, _seq(t, name, like.shape, like.dtype, like.device)
 
 
 def lru_forward(x, r, i, lam, h0=None, mask=None, reset=None, c=8.0, keep_states=True, out=None,
@@ -395,9 +400,9 @@ def lru_forward(x, r, i, lam, h0=None, mask=None, reset=None, c=8.0, keep_states
     shape, code, dv, (sx, sr, si) = _lru_inputs(x, r, i, lam, mask, reset)
     L, B, d = shape
     _req(h0, "h0", (B, d), optional=True, device=dv)
-    H, sh = _seq_out(out, "H", shape, x.dtype, dv)
-    h_last = _out(out, "h_last", (B, d), _F32, dv)
-    states = (_out(out, "states", (-(-L // LRU_STEPS), B, d), _F32, dv) if keep_states else None)
+    H, sh = _seq_out(out, "H", x)
+    h_last = _out(out, "h_last", (B, d), _F32, x)
+    states = _out(out, "states", (-(-L // LRU_STEPS), B, d), _F32, x) if keep_states else None
     lib = sru.lib()
     ws, nbytes = _ws(ws, lib.sru_lru_forward_workspace_bytes(L, B, d), dv)
     st = lib.sru_lru_forward(L, B, d, code, _ptr(x), *sx, _ptr(r), *sr, _ptr(i), *si, _ptr(lam), c,
@@ -417,11 +422,11 @@ def lru_backward(x, r, i, lam, states, dH, dh_last=None, mask=None, reset=None, 
     _req(states, "states", (-(-L // LRU_STEPS), B, d), device=dv)
     sdh = _seq(dH, "dH", shape, x.dtype, dv)
     _req(dh_last, "dh_last", (B, d), optional=True, device=dv)
-    dx, sdx = _seq_out(out, "dx", shape, x.dtype, dv)
-    dr, sdr = _seq_out(out, "dr", shape, x.dtype, dv)
-    di, sdi = _seq_out(out, "di", shape, x.dtype, dv)
-    dlam = _out(out, "dlam", (d,), _F32, dv)
-    dh0 = _out(out, "dh0", (B, d), _F32, dv) if want_dh0 else None
+    dx, sdx = _seq_out(out, "dx", x)
+    dr, sdr = _seq_out(out, "dr", x)
+    di, sdi = _seq_out(out, "di", x)
+    dlam = _out(out, "dlam", (d,), _F32, x)
+    dh0 = _out(out, "dh0", (B, d), _F32, x) if want_dh0 else None
     lib = sru.lib()
     ws, nbytes = _ws(ws, lib.sru_lru_backward_workspace_bytes(L, B, d), dv)
     st = lib.sru_lru_backward(L, B, d, code, _ptr(x), *sx, _ptr(r), *sr, _ptr(i), *si, _ptr(lam),
@@ -432,17 +437,37 @@ def lru_backward(x, r, i, lam, states, dH, dh_last=None, mask=None, reset=None, 
     return dict(dx=dx, dr=dr, di=di, dlam=dlam, dh0=dh0)
 
 
+def _step_rows(t, name, shape, dtype, device):
+    """The distance of sequences of a [B, d] tensor with contiguous features."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-d tensor [B, d]")
+    return _seq(t.unsqueeze(0), name, (1,) + tuple(shape), dtype, device)[1]
+
+
 def lru_step(x, r, i, lam, h, c=8.0, out=None):
     """One token of the recurrence: x, r, i [B, d], the state h [B, d] float32
     taken on in place.  Returns the output [B, d] (out, or a new tensor)."""
-    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+    code = _dtype(x, "x")
+    if x.dim() != 2:
         raise ValueError("x must be a 2-d tensor [B, d]")
-    if h is None:
-        raise ValueError("h is required")
-    one = [t.unsqueeze(0) if isinstance(t, torch.Tensor) else t for t in (x, r, i)]
+    dv, dt, shape = _here(x, "x"), x.dtype, x.shape
+    B, d = shape
+    fast = x.stride(1) == 1
+    for n, t in (("r", r), ("i", i)):
+        fast = (fast and t.__class__ is torch.Tensor and t.dtype is dt and t.shape == shape
+                and t.device == dv and t.stride(1) == 1)
+    if not fast:  # one by one, for the message
+        for n, t in (("x", x), ("r", r), ("i", i)):
+            _step_rows(t, n, shape, dt, dv)
+    _req(lam, "lam", (d,), device=dv)
+    _req(h, "h", (B, d), device=dv)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    elif not isinstance(out, torch.Tensor):
-        raise ValueError("out must be a torch tensor")
-    lru_forward(*one, lam, h, c=c, keep_states=False, out=dict(H=out.unsqueeze(0), h_last=h))
+        out, so = x.new_empty(shape), d
+    else:
+        so = _step_rows(out, "out", shape, dt, dv)
+    hp = _ptr(h)
+    st = sru.lib().sru_lru_forward(1, B, d, code, _ptr(x), 0, x.stride(0), _ptr(r), 0,
+                                   r.stride(0), _ptr(i), 0, i.stride(0), _ptr(lam), c, hp, None,
+                                   None, _ptr(out), 0, so, hp, None, None, 0, sru._stream())
+    _check(st, "sru_lru_forward")
     return out
