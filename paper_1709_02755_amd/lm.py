@@ -444,9 +444,11 @@ def _step_rows(t, name, shape, dtype, device):
     return _seq(t.unsqueeze(0), name, (1,) + tuple(shape), dtype, device)[1]
 
 
-def lru_step(x, r, i, lam, h, c=8.0, out=None):
+def lru_step(x, r, i, lam, h, c=8.0, out=None, mask=None, reset=None):
     """One token of the recurrence: x, r, i [B, d], the state h [B, d] float32
-    taken on in place.  Returns the output [B, d] (out, or a new tensor)."""
+    taken on in place.  mask and reset [B] uint8 as in lru_forward: a stream
+    without a token (its state stays, its output is 0), one that starts a new
+    document.  Returns the output [B, d] (out, or a new tensor)."""
     code = _dtype(x, "x")
     if x.dim() != 2:
         raise ValueError("x must be a 2-d tensor [B, d]")
@@ -461,13 +463,16 @@ def lru_step(x, r, i, lam, h, c=8.0, out=None):
             _step_rows(t, n, shape, dt, dv)
     _req(lam, "lam", (d,), device=dv)
     _req(h, "h", (B, d), device=dv)
+    _req(mask, "mask", (B,), dtype=torch.uint8, optional=True, device=dv)
+    _req(reset, "reset", (B,), dtype=torch.uint8, optional=True, device=dv)
     if out is None:
         out, so = x.new_empty(shape), d
     else:
         so = _step_rows(out, "out", shape, dt, dv)
     hp = _ptr(h)
     st = sru.lib().sru_lru_forward(1, B, d, code, _ptr(x), 0, x.stride(0), _ptr(r), 0,
-                                   r.stride(0), _ptr(i), 0, i.stride(0), _ptr(lam), c, hp, None,
-                                   None, _ptr(out), 0, so, hp, None, None, 0, sru._stream())
+                                   r.stride(0), _ptr(i), 0, i.stride(0), _ptr(lam), c, hp,
+                                   _ptr(mask), _ptr(reset), _ptr(out), 0, so, hp, None, None, 0,
+                                   sru._stream())
     _check(st, "sru_lru_forward")
     return out

@@ -236,6 +236,19 @@ def test_single_tokens_and_cut_calls(dtype):
     close("dh0", ga["dh0"], ref["h0"])
 
 
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_single_tokens_with_mask_and_reset(dtype):
+    L, B, d = 40, 5, 70
+    t = inputs(L, B, d, dtype, 12, mask=True, reset=True)
+    H, h_last, _, _ = plain(t)
+    v = dev(t)
+    h = v["h0"].clone()
+    rows = [lm.lru_step(v["x"][k], v["r"][k], v["i"][k], v["lam"], h, c=C, mask=v["mask"][k],
+                        reset=v["reset"][k]) for k in range(L)]
+    close("H", torch.stack(rows), H)
+    close("h", h, h_last)
+
+
 def test_what_does_not_count_reaches_nothing():
     """NaN and infinity at padded steps, in a wholly padded sequence and before a
     new document."""

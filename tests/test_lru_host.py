@@ -146,6 +146,8 @@ def test_binding(stub):
         lambda: lm.lru_step(x[0], x[0], x[0], lam, h.to(B16)),
         lambda: lm.lru_step(x[0], x[0], x[0], lam, None),
         lambda: lm.lru_step(x[0], x[0], x[0], lam, h, out=h),
+        lambda: lm.lru_step(x[0], x[0], x[0], lam, h, mask=m),
+        lambda: lm.lru_step(x[0], x[0], x[0], lam, h, reset=m[0].bool()),
     ]
     for i, call in enumerate(bad):
         with pytest.raises(ValueError):
