@@ -1,0 +1,227 @@
+"""A small recurrent language model on the library's operators, end to end:
+distilled from a teacher's best tokens, scored on held-out text, and run token
+by token.
+
+    python examples/recurrent_lm.py [--steps 200] [--width 256] [--vocab 2048]
+
+A block is norm -> one projection to (x, r, i, z) -> gated linear recurrence over
+(x, r, i) -> norm, gate by z and scaled residual.  The call that ends a block
+also makes the next block's normed input, so nothing else runs between the
+products.  Text and teacher are synthetic: a random Markov chain writes the
+documents, which are packed one after the other (token 0 starts each), and its
+transition logits are the teacher's.
+"""
+
+from __future__ import annotations
+
+import argparse
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+from paper_1709_02755_amd import lm, sru  # noqa: E402
+
+
+class RecurrentLM:
+    """Parameters by name in `self.p`; gradients by the same names from
+    `backward`."""
+
+    def __init__(self, vocab, width, blocks, device, gemm_dtype=sru.GEMM_BF16, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        self.vocab, self.width, self.blocks, self.gemm = vocab, width, blocks, gemm_dtype
+
+        def normal(*shape, std):
+            return (torch.randn(shape, generator=g) * std).to(device)
+
+        def ones(scale=1.0):
+            return torch.full((width,), scale, device=device)
+
+        p = dict(embed=normal(vocab, width, std=1.0), head=normal(vocab, width, std=width ** -0.5),
+                 pre0=ones())
+        for n in range(blocks):
+            p[f"proj{n}"] = normal(4 * width, width, std=width ** -0.5)
+            # a^(1/sigma(r)) from 0.9 to 0.999 at c = 8
+            a = torch.linspace(0.9, 0.999, width, dtype=torch.float64)
+            p[f"lam{n}"] = torch.log(torch.expm1(-torch.log(a) / 8)).float().to(device)
+            p[f"post{n}"], p[f"scale{n}"], p[f"pre{n + 1}"] = ones(), ones(0.5), ones()
+        self.p = p
+
+    def new_state(self, B):
+        """The state of B streams, per block; forward and step take it on."""
+        return [torch.zeros(B, self.width, device=self.p["embed"].device)
+                for _ in range(self.blocks)]
+
+    def forward(self, tokens, state=None, keep=False):
+        """Logits [L * B, V] of tokens [L, B], and what backward needs."""
+        p, (L, B), d = self.p, tokens.shape, self.width
+        reset = (tokens == 0).to(torch.uint8)
+        x = p["embed"][tokens]
+        o = lm.residual_norm_forward(x, w_pre=p["pre0"])
+        saved = dict(tokens=tokens, reset=reset, x0=x, rstd0=o["rstd"], blocks=[])
+        o = o["o"]
+        for n in range(self.blocks):
+            u = sru.gemm(sru.OP_NT, o.view(L * B, d), p[f"proj{n}"], L * B, 4 * d, d, self.gemm)
+            u = u.view(L, B, 4, d)
+            f = lm.lru_forward(u[:, :, 0], u[:, :, 1], u[:, :, 2], p[f"lam{n}"],
+                               h0=None if state is None else state[n], reset=reset,
+                               keep_states=keep)
+            if state is not None:
+                state[n] = f["h_last"]
+            e = lm.residual_norm_forward(x, f["H"], p[f"post{n}"], u[:, :, 3], p[f"scale{n}"],
+                                         p[f"pre{n + 1}"])
+            if keep:
+                saved["blocks"].append(dict(o=o, u=u, x=x, H=f["H"], states=f["states"],
+                                            rstd=e["rstd"]))
+            x, o = e["x_out"], e["o"]
+        saved["o"] = o
+        logits = sru.gemm(sru.OP_NT, o.view(L * B, d), p["head"], L * B, self.vocab, d, self.gemm)
+        return logits, saved
+
+    def backward(self, saved, dlogits):
+        """Gradients of the parameters."""
+        p, d, V = self.p, self.width, self.vocab
+        L, B = saved["tokens"].shape
+        N, g = L * B, {}
+        g["head"] = sru.gemm(sru.OP_TN, dlogits, saved["o"].view(N, d), V, d, N, self.gemm)
+        do = sru.gemm(sru.OP_NN, dlogits, p["head"], N, d, V, self.gemm).view(L, B, d)
+        dx = None
+        for n in reversed(range(self.blocks)):
+            s = saved["blocks"][n]
+            du = torch.empty_like(s["u"])
+            e = lm.residual_norm_backward(s["x"], s["H"], s["rstd"], dx, do, p[f"post{n}"],
+                                          s["u"][:, :, 3], p[f"scale{n}"], p[f"pre{n + 1}"],
+                                          out=dict(dz=du[:, :, 3]))
+            f = lm.lru_backward(s["u"][:, :, 0], s["u"][:, :, 1], s["u"][:, :, 2], p[f"lam{n}"],
+                                s["states"], e["dy"], reset=saved["reset"], want_dh0=False,
+                                out=dict(dx=du[:, :, 0], dr=du[:, :, 1], di=du[:, :, 2]))
+            g[f"post{n}"], g[f"scale{n}"], g[f"pre{n + 1}"] = e["dw_post"], e["dscale"], e["dw_pre"]
+            g[f"lam{n}"], du = f["dlam"], du.view(N, 4 * d)
+            g[f"proj{n}"] = sru.gemm(sru.OP_TN, du, s["o"].view(N, d), 4 * d, d, N, self.gemm)
+            do = sru.gemm(sru.OP_NN, du, p[f"proj{n}"], N, d, 4 * d, self.gemm).view(L, B, d)
+            dx = e["dx"]
+        e = lm.residual_norm_backward(saved["x0"], None, saved["rstd0"], dx, do, w_pre=p["pre0"])
+        g["pre0"] = e["dw_pre"]
+        g["embed"] = torch.zeros_like(p["embed"])
+        g["embed"].index_put_((saved["tokens"].reshape(-1),), e["dx"].view(N, d), accumulate=True)
+        return g
+
+    def step(self, tokens, state):
+        """Logits [B, V] after one more token per stream; the state is taken on
+        in place."""
+        p, B, d = self.p, tokens.shape[0], self.width
+        reset = (tokens == 0).to(torch.uint8)
+        x = p["embed"][tokens]
+        o = lm.residual_norm_forward(x, w_pre=p["pre0"])["o"]
+        for n in range(self.blocks):
+            u = sru.gemm(sru.OP_NT, o, p[f"proj{n}"], B, 4 * d, d, self.gemm).view(B, 4, d)
+            h = lm.lru_step(u[:, 0], u[:, 1], u[:, 2], p[f"lam{n}"], state[n], reset=reset)
+            e = lm.residual_norm_forward(x, h, p[f"post{n}"], u[:, 3], p[f"scale{n}"],
+                                         p[f"pre{n + 1}"])
+            x, o = e["x_out"], e["o"]
+        return sru.gemm(sru.OP_NT, o, p["head"], B, self.vocab, d, self.gemm)
+
+    def distill(self, tokens, teacher_ids, teacher_logits, temperature=1.0):
+        """Mean loss against the teacher's entries [L * B, K], and gradients."""
+        logits, saved = self.forward(tokens, keep=True)
+        each = torch.full((logits.shape[0],), 1.0 / logits.shape[0], device=logits.device)
+        r = lm.distill_forward_backward(logits, teacher_ids, teacher_logits, each, temperature,
+                                        dlogits=logits)
+        return r["loss"].mean(), self.backward(saved, r["dlogits"])
+
+    def fit(self, tokens, targets):
+        """Mean negative log probability of targets [L, B], and gradients."""
+        logits, saved = self.forward(tokens, keep=True)
+        want = targets.reshape(-1)
+        r = lm.token_logprobs(logits, want)
+        each = torch.full_like(r["logprob"], -1.0 / want.numel())
+        dlogits = lm.token_logprobs_backward(logits, want, r, dlogprob=each, dlogits=logits)
+        return -r["logprob"].mean(), self.backward(saved, dlogits)
+
+    def score(self, tokens, targets, state=None, top=0):
+        """token_logprobs of targets [L, B] after tokens [L, B]."""
+        return lm.token_logprobs(self.forward(tokens, state)[0], targets.reshape(-1), top)
+
+    def generate(self, first, count, state, temperature=1.0, top=20, generator=None):
+        """`count` tokens per stream after `first` [B], each drawn among the
+        `top` best; returns (tokens [count, B], their log probabilities over the
+        whole vocabulary [count, B])."""
+        tokens, said, logps = first, [], []
+        for _ in range(count):
+            r = lm.token_logprobs(self.step(tokens, state), tokens, top, temperature)
+            pick = torch.multinomial(r["top_logprobs"].exp(), 1, generator=generator)
+            tokens = r["top_ids"].gather(1, pick).squeeze(1)
+            said.append(tokens)
+            logps.append(r["top_logprobs"].gather(1, pick).squeeze(1))
+        return torch.stack(said), torch.stack(logps)
+
+
+class Source:
+    """Documents of a random Markov chain: each token has `fan` successors, and
+    any token may end its document (0 starts the next)."""
+
+    def __init__(self, vocab, fan, device, seed=1):
+        self.g = torch.Generator(device).manual_seed(seed)
+        self.ids = torch.randint(1, vocab, (vocab, fan), generator=self.g, device=device)
+        self.ids[:, 0] = 0  # the end of a document
+        self.logits = torch.randn(vocab, fan, generator=self.g, device=device)
+        self.logits[:, 0] -= 3.0
+
+    def batch(self, L, B):
+        """(tokens [L, B], targets [L, B], teacher's ids and logits [L * B, fan])."""
+        probs, t = self.logits.softmax(1), torch.zeros(B, dtype=torch.int64, device=self.ids.device)
+        said = [t]
+        for _ in range(L):
+            pick = torch.multinomial(probs[t], 1, generator=self.g)
+            t = self.ids[t].gather(1, pick).squeeze(1)
+            said.append(t)
+        s = torch.stack(said)
+        at = s[:-1].reshape(-1)
+        return s[:-1].contiguous(), s[1:].contiguous(), self.ids[at], self.logits[at]
+
+
+def main():
+    a = argparse.ArgumentParser()
+    a.add_argument("--steps", type=int, default=200)
+    a.add_argument("--width", type=int, default=256)
+    a.add_argument("--vocab", type=int, default=2048)
+    a.add_argument("--blocks", type=int, default=2)
+    a.add_argument("--length", type=int, default=128)
+    a.add_argument("--streams", type=int, default=32)
+    a = a.parse_args()
+    dev = torch.device("cuda:0")
+    model = RecurrentLM(a.vocab, a.width, a.blocks, dev)
+    source = Source(a.vocab, 16, dev)
+    opt = torch.optim.Adam(model.p.values(), lr=3e-3)
+
+    def update(grads):
+        for n, t in model.p.items():
+            t.grad = grads[n]
+        opt.step()
+
+    for n in range(a.steps):
+        tokens, targets, ids, logits = source.batch(a.length, a.streams)
+        if n < a.steps // 2:
+            loss, grads = model.distill(tokens, ids, logits)
+        else:
+            loss, grads = model.fit(tokens, targets)
+        update(grads)
+        if n % max(1, a.steps // 10) == 0 or n == a.steps - 1:
+            kind = "distill" if n < a.steps // 2 else "tokens"
+            print(f"step {n:4d} {kind:8s} loss {float(loss):.4f}", flush=True)
+    tokens, targets, ids, logits = source.batch(a.length, a.streams)
+    r = model.score(tokens, targets)
+    best = lm.token_logprobs(logits, (ids == targets.reshape(-1, 1)).to(torch.int64).argmax(1))
+    print(f"held out: {-float(r['logprob'].mean()):.4f} nats per token "
+          f"(the source itself: {-float(best['logprob'].mean()):.4f}), "
+          f"entropy {float(r['entropy'].mean()):.4f}")
+    first = torch.zeros(4, dtype=torch.int64, device=dev)
+    said, logps = model.generate(first, 12, model.new_state(4))
+    for b in range(4):
+        print("stream", b, said[:, b].tolist(), f"{-float(logps[:, b].mean()):.3f} nats per token")
+
+
+if __name__ == "__main__":
+    main()
