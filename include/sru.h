@@ -466,9 +466,9 @@ SRU_API int sru_residual_norm_backward(int M, int d, int dtype, int res_dtype, i
  *   states [ceil(L / SRU_LRU_STEPS), B, d]: the state before every
  *     SRU_LRU_STEPS-th step, which the gradient call reads (it reads no H);
  *     NULL in the forward: inference
- * One step with h0 = h_last is the form for single tokens.  Sequences of more
- * than 64 steps are cut into segments, each one workgroup's, whose maps meet in
- * the workspace; the results do not depend on the order in which they ran.
+ * One step with h0 = h_last is the form for single tokens.  Long sequences of
+ * few channels are cut into chunks whose maps go through the workspace; results
+ * are the same in every run.
  * A sequence cut into consecutive calls (h_last -> h0) agrees with one call to
  * fp32 rounding. */
 #define SRU_LRU_STEPS 8
@@ -513,7 +513,7 @@ SRU_API int sru_lru_backward(int L, int B, int d, int dtype, const void* x, long
  *     "distill_grad";
  *   residual norm: "norm", "norm_grad", "norm_sums" (parameter gradients);
  *   gated linear recurrence: "lru", "lru_grad", "lru_sums" (gradient of lam),
- *     "lru_clear" (the segments' words, with several segments).
+ *     "lru_maps", "lru_grad_maps" (of the chunks of long sequences).
  * The caller owns the events and reads them after synchronising.
  * Disarmed (the default), launches record nothing.
  * ------------------------------------------------------------------------- */

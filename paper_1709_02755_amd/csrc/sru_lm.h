@@ -104,8 +104,7 @@ size_t norm_grad_workspace_bytes(int M, int d);
 hipError_t norm_grad_launch(const NormArgs& a, hipStream_t stream);
 
 // ------------------------------------------------- gated linear recurrence
-constexpr int kLruSteps = 8;     // a state is kept for so many steps, a wave's of the gradient
-constexpr int kLruForward = 8;   // steps a wave holds in the forward
+constexpr int kLruSteps = 8;  // the steps that a wave holds, and that a state is kept for
 
 // [L, B, d] with contiguous features; distances of steps and of sequences in
 // elements.
@@ -135,7 +134,7 @@ struct LruArgs {
 };
 size_t lru_workspace_bytes(int L, int B, int d);
 size_t lru_grad_workspace_bytes(int L, int B, int d);
-// Workgroups of a call (they must fit a launch).
+// Workgroups of a call, at most (they must fit a launch).
 long long lru_blocks(int L, int B, int d);
 hipError_t lru_launch(const LruArgs& a, hipStream_t stream);
 hipError_t lru_grad_launch(const LruArgs& a, hipStream_t stream);

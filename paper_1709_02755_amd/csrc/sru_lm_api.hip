@@ -114,7 +114,8 @@ struct SeqCheck {
 int check_lru(int L, int B, int d, int dtype, float c) {
   if (!valid_dtype(dtype)) return SRU_E_FLAG;
   if (L <= 0 || B <= 0 || d <= 0) return SRU_E_SHAPE;
-  if ((long long)B * d > INT_MAX || (long long)L * B > INT_MAX) return SRU_E_SHAPE;
+  if ((long long)B * d > INT_MAX || (long long)L * B > INT_MAX - 1024) return SRU_E_SHAPE;
+  if ((long long)B * d > kMaxElems / L) return SRU_E_SHAPE;
   // 1024 threads a workgroup, below 2^32 in a launch
   if (sru::lru_blocks(L, B, d) >= 1LL << 22) return SRU_E_SHAPE;
   if (!std::isfinite(c) || c < 0.f) return SRU_E_SHAPE;

@@ -11,12 +11,25 @@
 //   dlam = -c sigma(lam) sum_t dla s,  dh0 = c_0
 //
 // A step is an affine map of the state, h -> A h + B, and so is any run of
-// steps; both directions are one scan over such maps.  A wave holds some
-// steps (kLruForward or kLruSteps) of 64 lanes, VEC channels each, in registers,
-// a workgroup up to kLruWaves
-// waves, consecutive in time: a segment.  Maps are joined in the workgroup
-// through LDS and, where a sequence has several segments, across workgroups
-// through one 64-bit word per channel and segment: everything is read once.
+// steps; both directions are one scan over such maps.  A wave holds kLruSteps
+// steps of 64 lanes, VEC channels each, in registers, and a workgroup's waves,
+// consecutive in time, a segment.  Their maps meet in LDS: each wave gets the state
+// that enters its steps, runs them and writes.  A workgroup goes through the
+// segments of its channels in turn and loads the next one while it finishes
+// this one, so everything is read once.  Where that leaves most of the GPU idle
+// (few channels, a long sequence), a sequence is cut into chunks of segments: one
+// kernel folds all chunks but the last into their maps, and then each chunk's
+// workgroup starts from the maps before it.  No workgroup waits for another one,
+// and the results do not depend on when which one ran.
+//
+// What bounds it: memory, with the gates' arithmetic close behind (39 vector
+// instructions an element forward, 5 of them exp, rcp or sqrt; the vector units are
+// busy 46 % of the time forward, 50 % of the gradient's).  L 256, B 64, d 1024 in
+// bf16: 32 us for 134 MB (4.2 TB/s) and 61 us for 235 MB (3.9), where a large copy
+// makes 5.4.  L 32768, B 1, d 1024: 110 us and 143 us, for three quarters more to
+// read forward and a third more in the gradient than in one pass; workgroups that
+// handed on their state to the next one through memory read everything once, but
+// took 114 and 171 us: a state needs 2 to 3 us from one workgroup to the next.
 //
 // A map with A = 0 forgets what came before: that is how a new document's
 // start, and a state that is known, are written (a state of NaN before a new
@@ -31,8 +44,8 @@ namespace sru {
 namespace {
 
 constexpr int T = kLruSteps;
-constexpr int kLook = 8;   // segments of a block
-constexpr int kFewChannels = 4096;
+constexpr int kWaves = 8, kGradWaves = 4;          // of a workgroup
+constexpr int kWideWaves = 16, kWideGradWaves = 8;  // of one with one channel a lane, unchunked
 constexpr float kTiny = 1.17549435e-38f;
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -131,38 +144,54 @@ struct Ptr {
   }
 };
 
-// A tensor's packed values at a wave's N steps from t0, zeros where there are none.
-template <bool BF16, int VEC, int N>
+// A tensor's packed values at a wave's T steps from t0, zeros where there are none.
+template <bool BF16, int VEC>
 __device__ __forceinline__ void load_steps(const LruArgs& a, const Seq& s, const Lane& n, int t0,
-                                           Pack<BF16, VEC> (&x)[N]) {
+                                           Pack<BF16, VEC> (&x)[T]) {
   const Ptr<BF16, VEC> p(s, n, t0);
 #pragma unroll
-  for (int u = 0; u < N; ++u) x[u] = Pack<BF16, VEC>{};
+  for (int u = 0; u < T; ++u) x[u] = Pack<BF16, VEC>{};
   if (!n.live) return;
-  if (t0 + N <= a.L) {
+  if (t0 + T <= a.L) {
 #pragma unroll
-    for (int u = 0; u < N; ++u) x[u] = p.load(u);
+    for (int u = 0; u < T; ++u) x[u] = p.load(u);
   } else {
 #pragma unroll
-    for (int u = 0; u < N; ++u)
+    for (int u = 0; u < T; ++u)
       if (t0 + u < a.L) x[u] = p.load(u);
   }
 }
 
-// What a wave knows of its N steps: how many there are, and bit u of pad, fresh
-// for step u.  Lane u reads step u's marks.
+// Lane u's marks of the wave's step u, as they are in memory.
+struct Marks {
+  unsigned pad, fresh;
+};
+template <bool FLAGS>
+__device__ __forceinline__ Marks load_marks(const LruArgs& a, const Lane& n, int t0) {
+  Marks m{0, 0};
+  if constexpr (FLAGS) {
+    const int u = threadIdx.x & 63;
+    if (u < T && t0 + u < a.L) {
+      const long long o = (long long)(t0 + u) * a.B + n.b;
+      if (a.mask) m.pad = a.mask[o];
+      if (a.reset) m.fresh = a.reset[o];
+    }
+  }
+  return m;
+}
+
+// What a wave knows of its T steps: how many there are, and bit u of pad, fresh
+// for step u.
 struct Flags {
   int count;
   unsigned pad, fresh;
 };
-template <bool FLAGS, int N>
-__device__ __forceinline__ Flags flags_of(const LruArgs& a, const Lane& n, int t0) {
-  Flags f{min(max(a.L - t0, 0), N), 0, 0};
+template <bool FLAGS>
+__device__ __forceinline__ Flags flags_of(const LruArgs& a, int t0, const Marks& m) {
+  Flags f{min(max(a.L - t0, 0), T), 0, 0};
   if constexpr (FLAGS) {
-    const int u = threadIdx.x & 63;
-    const long long o = (long long)(t0 + u) * a.B + n.b;
-    if (a.mask) f.pad = (unsigned)__ballot(u < f.count && a.mask[o] != 0);
-    if (a.reset) f.fresh = (unsigned)__ballot(u < f.count && a.reset[o] != 0) & ~f.pad;
+    f.pad = (unsigned)__ballot(m.pad != 0);
+    f.fresh = (unsigned)__ballot(m.fresh != 0) & ~f.pad;
   }
   return f;
 }
@@ -203,191 +232,118 @@ __device__ __forceinline__ float decay_rate(const LruArgs& a, int j) {
   const float l = a.lam[j];
   return a.c * (fmaxf(l, 0.f) + log1pf(expf(-fabsf(l))));
 }
-// k of the lane's channels.  With several segments the call's first kernel has
-// worked them out; else the first wave does, for all.  Returns whether all of
-// the wave's series converge (s <= 1).
+// k of the lane's channels: the first wave works them out for all.  Returns
+// whether all of the wave's series converge (s <= 1).
 template <int VEC>
-__device__ __forceinline__ bool decay_rates(const LruArgs& a, const float* rates, const Lane& n,
-                                            float* lds, float (&k)[VEC]) {
-  if (rates) {
+__device__ __forceinline__ bool decay_rates(const LruArgs& a, const Lane& n, float* lds,
+                                            float (&k)[VEC]) {
+  if (threadIdx.x < 64) {
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) k[v] = n.live ? rates[n.j + v] : 0.f;
-  } else {
-    if (threadIdx.x < 64) {
-#pragma unroll
-      for (int v = 0; v < VEC; ++v)
-        lds[v * 64 + threadIdx.x] = n.live ? decay_rate(a, n.j + v) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) k[v] = lds[v * 64 + (threadIdx.x & 63)];
+    for (int v = 0; v < VEC; ++v)
+      lds[v * 64 + threadIdx.x] = n.live ? decay_rate(a, n.j + v) : 0.f;
   }
+  __syncthreads();
   bool beyond = false;
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) beyond |= !(k[v] < kSeriesEnd);
+  for (int v = 0; v < VEC; ++v) {
+    k[v] = lds[v * 64 + (threadIdx.x & 63)];
+    beyond |= !(k[v] < kSeriesEnd);
+  }
   return !__any(beyond);
 }
 
-// ------------------------------------------------------ maps across segments
-// One word per channel and segment: a map (A in the upper half), all ones
-// while there is none.  A is never NaN, so no map looks like that.
-constexpr unsigned long long kEmpty = ~0ull;
-__device__ __forceinline__ unsigned long long word_of(Map m) {
-  return ((unsigned long long)__float_as_uint(m.A) << 32) | __float_as_uint(m.B);
-}
-__device__ __forceinline__ Map map_of(unsigned long long w) {
-  return Map{__uint_as_float((unsigned)(w >> 32)), __uint_as_float((unsigned)w)};
-}
-
-struct Chain {
-  unsigned* tickets;          // one a lane group, kTicketPitch apart
-  unsigned long long* words;  // [nseg, B * d]
-  float* rates;               // [d]; nullptr with one segment
-  int nseg, groups;
+// A segment is what a workgroup's waves hold at a time, a chunk the segments
+// that one workgroup goes through, both counted in the order of the scan.
+struct Cut {
+  Map* maps;  // [chunks - 1, B * d]
+  int nseg, each, chunks, groups;  // segments, those of a chunk, chunks, lane groups
 };
-constexpr int kTicketPitch = 16;  // a cache line each: all start at the same time
 
-// The segment (in the order of the scan) that a workgroup of a lane group takes:
-// tickets are handed out as workgroups start, and a segment only waits for
-// those with lower tickets.  These have started, so they get on whatever else
-// waits: every wait ends.
-__device__ __forceinline__ int take_ticket(const Chain& c, int group, unsigned* lds) {
-  if (c.nseg == 1) return 0;
-  if (threadIdx.x == 0)
-    *lds = __hip_atomic_fetch_add(c.tickets + (long long)group * kTicketPitch, 1u,
-                                  __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  return __builtin_amdgcn_readfirstlane(*lds);
-}
+// What the waves of a workgroup share: there are two sets of maps in turn, so
+// that a segment takes one barrier.
+template <int VEC, int W>
+struct Shared {
+  Map maps[2][W * VEC * 64];  // of the waves, in the order of the scan
+  float rates[VEC * 64];
+};
 
-template <int VEC>
-__device__ __forceinline__ void publish(const Chain& c, const LruArgs& a, const Lane& n, int rank,
-                                        const Map (&m)[VEC]) {
-  if (!n.live) return;
-  unsigned long long* w = c.words + (long long)rank * a.B * a.d + n.chan;
+// Turns the state that enters the sequence into the one that enters the chunk, by
+// the maps of the chunks before it: a wave joins a run of them, and all waves
+// those joined.
+template <int VEC, int W>
+__device__ __forceinline__ void enter_chunk(const LruArgs& a, const Cut& c, const Lane& n,
+                                            int chunk, Shared<VEC, W>& sh, float (&in)[VEC]) {
+  if (chunk == 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int run = (chunk + W - 1) / W, last = min(chunk, (wave + 1) * run);
+  const long long lanes = (long long)a.B * a.d;
+  Map m[VEC];
 #pragma unroll
-  for (int v = 0; v < VEC; ++v)
-    __hip_atomic_store(w + v, word_of(m[v]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-// The map in a word once it is there.  The wait ends by the order of the tickets;
-// its bound (seconds) keeps a mistake there from hanging the GPU: NaN then.
-__device__ __forceinline__ Map wait_for(const unsigned long long* word, bool live) {
-  unsigned long long x = kEmpty;
-#pragma unroll 1
-  for (int spin = 0; live && spin < (1 << 22); ++spin) {
-    x = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (x != kEmpty) break;
-    __builtin_amdgcn_s_sleep(1);
+  for (int v = 0; v < VEC; ++v) m[v] = Map{1.f, 0.f};
+#pragma unroll 4
+  for (int e = wave * run; e < last; ++e) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v)
+      if (n.live) m[v] = join(c.maps[e * lanes + n.chan + v], m[v]);
   }
-  return map_of(x);
+  if (wave * run < chunk) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) sh.maps[1][(wave * VEC + v) * 64 + lane] = m[v];
+  }
+  __syncthreads();
+  for (int w = 0; w * run < chunk; ++w)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) in[v] = apply(sh.maps[1][(w * VEC + v) * 64 + lane], in[v]);
 }
 
-// The maps of a workgroup's waves, in LDS in the order of the scan (`place` of
-// a wave's steps in it), joined: the state that enters the wave's steps, and
-// the segment's map where the state entering that is not known yet.
+// The state that enters the wave's steps (`place` in the order of the scan) from
+// the one that enters the segment, which becomes the next segment's.
 template <int U, int VEC>
-__device__ __forceinline__ void enter_wave(const Map* maps, int place, const float (&seg_in)[VEC],
-                                           float (&in)[VEC]) {
+__device__ __forceinline__ void enter_wave(const Map* maps, int place, int waves,
+                                           float (&seg_in)[VEC], float (&in)[VEC]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int v = 0; v < VEC; ++v) in[v] = seg_in[v];
 #pragma unroll U
-  for (int w = 0; w < place; ++w)
+  for (int w = 0; w < waves; ++w)
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) in[v] = apply(maps[(w * VEC + v) * 64 + lane], in[v]);
+    for (int v = 0; v < VEC; ++v) {
+      if (w == place) in[v] = seg_in[v];
+      seg_in[v] = apply(maps[(w * VEC + v) * 64 + lane], seg_in[v]);
+    }
 }
 
-// The state that enters the segment; `first` is what enters rank 0.  Segments
-// come in blocks of kLook.  The last one of a block leaves the state after the
-// block (a map with A = 0) in its word, the others their own map; a segment
-// takes the state before its block and the maps of its block before it.  All
-// are joined in the order of the scan, the state last of all, so that a state
-// passes a block in one hop of a word, and the result does not depend on which
-// workgroup ran when.  win: kLook * 64 * VEC maps.
-// U: how far the loops over maps are unrolled (their reads take registers).
-template <int U, int VEC>
-__device__ __forceinline__ void join_segments(const Chain& c, const LruArgs& a, const Lane& n,
-                                              int rank, int waves, const Map* maps, Map* win,
-                                              const float (&first)[VEC], float (&seg_in)[VEC]) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// A chunk's map, from those of the waves.
+template <int VEC, int W>
+__device__ __forceinline__ void chunk_map(const LruArgs& a, const Cut& c, const Lane& n, int chunk,
+                                          int place, Shared<VEC, W>& sh, Map (&m)[VEC]) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) seg_in[v] = first[v];
-  if (c.nseg == 1) return;
-  const int inside = rank % kLook, block = rank - inside;
-  const bool mine = wave == 0 && rank + 1 < c.nseg, leaves = inside == kLook - 1;
-  const long long lanes = (long long)a.B * a.d;
-  unsigned long long* const words = c.words + n.chan;
-  Map seg[VEC];
-  if (mine) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) seg[v] = maps[v * 64 + lane];
-#pragma unroll U
-    for (int w = 1; w < waves; ++w)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) seg[v] = join(maps[(w * VEC + v) * 64 + lane], seg[v]);
-    if (!leaves) publish<VEC>(c, a, n, rank, seg);
-  }
-  if (rank == 0) return;
-#pragma unroll 1
-  for (int e = wave; e < inside; e += waves) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v)
-      win[(e * VEC + v) * 64 + lane] = wait_for(words + (block + e) * lanes + v, n.live);
-  }
+  for (int v = 0; v < VEC; ++v) sh.maps[0][(place * VEC + v) * 64 + lane] = m[v];
   __syncthreads();
-  if (mine && leaves) {
-    // the whole block as one map, before the state is there
-    Map all[VEC];
+  if (place != 0 || !n.live) return;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) all[v] = win[v * 64 + lane];
-#pragma unroll U
-    for (int e = 1; e < inside; ++e)
+  for (int w = 1; w < W; ++w)
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) all[v] = join(win[(e * VEC + v) * 64 + lane], all[v]);
+    for (int v = 0; v < VEC; ++v) m[v] = join(sh.maps[0][(w * VEC + v) * 64 + lane], m[v]);
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) seg[v] = join(seg[v], all[v]);
-  }
-  if (block > 0) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v)
-      seg_in[v] = wait_for(words + (block - 1) * lanes + v, n.live).B;
-  }
-  if (mine && leaves) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) seg[v] = Map{0.f, apply(seg[v], seg_in[v])};
-    publish<VEC>(c, a, n, rank, seg);
-  }
-#pragma unroll U
-  for (int e = 0; e < inside; ++e)
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) seg_in[v] = apply(win[(e * VEC + v) * 64 + lane], seg_in[v]);
-}
-
-// Empties the words (two at a time) and the tickets and works out the rates.
-__global__ __launch_bounds__(256) void lru_clear_kernel(LruArgs a, Chain c, long long pairs) {
-  const long long step = (long long)gridDim.x * 256;
-  const long long first = (long long)blockIdx.x * 256 + threadIdx.x;
-  ulonglong2* w = reinterpret_cast<ulonglong2*>(c.words);
-  for (long long i = first; i < pairs; i += step) w[i] = make_ulonglong2(kEmpty, kEmpty);
-  for (long long i = first; i < (long long)c.groups * kTicketPitch; i += step) c.tickets[i] = 0;
-  for (long long i = first; i < a.d; i += step) c.rates[i] = decay_rate(a, (int)i);
+  for (int v = 0; v < VEC; ++v) c.maps[chunk * ((long long)a.B * a.d) + n.chan + v] = m[v];
 }
 
 // -------------------------------------------------------------------- forward
 // A wave's steps as maps h -> A h + B (A of a document's first step is 0), and
 // the map of them all.  FLAGS: some step may be missing, be padded or start a
 // document.
-template <bool FLAGS, bool SERIES, bool BF16, int VEC, int N>
-__device__ __forceinline__ void step_maps(const Pack<BF16, VEC> (&x)[N],
-                                          const Pack<BF16, VEC> (&r)[N],
-                                          const Pack<BF16, VEC> (&i)[N], const float (&k)[VEC],
-                                          const Flags& f, float (&A)[N][VEC], float (&Bv)[N][VEC],
+template <bool FLAGS, bool SERIES, bool BF16, int VEC>
+__device__ __forceinline__ void step_maps(const Pack<BF16, VEC> (&x)[T],
+                                          const Pack<BF16, VEC> (&r)[T],
+                                          const Pack<BF16, VEC> (&i)[T], const float (&k)[VEC],
+                                          const Flags& f, float (&A)[T][VEC], float (&Bv)[T][VEC],
                                           Map (&all)[VEC]) {
 #pragma unroll
   for (int v = 0; v < VEC; ++v) all[v] = Map{1.f, 0.f};
 #pragma unroll
-  for (int u = 0; u < N; ++u) {
+  for (int u = 0; u < T; ++u) {
     if (FLAGS && u >= f.count) continue;
     const bool pad = FLAGS && (f.pad >> u & 1), fresh = FLAGS && (f.fresh >> u & 1);
 #pragma unroll
@@ -407,20 +363,19 @@ __device__ __forceinline__ void step_maps(const Pack<BF16, VEC> (&x)[N],
 }
 
 // The outputs of the steps once the state entering them is known.
-template <bool FLAGS, bool BF16, int VEC, int N>
+template <bool FLAGS, bool BF16, int VEC>
 __device__ __forceinline__ void run_steps(const LruArgs& a, const Lane& n, int t0, const Flags& f,
-                                          const float (&A)[N][VEC], const float (&Bv)[N][VEC],
+                                          const float (&A)[T][VEC], const float (&Bv)[T][VEC],
                                           float (&h)[VEC]) {
   const Ptr<BF16, VEC> out(a.h, n, t0);
-  float* kept = a.states ? a.states + (long long)(t0 / T) * a.B * a.d + n.chan : nullptr;
+  if (a.states) {
 #pragma unroll
-  for (int u = 0; u < N; ++u) {
+    for (int v = 0; v < VEC; ++v) a.states[(long long)(t0 / T) * a.B * a.d + n.chan + v] = h[v];
+  }
+#pragma unroll
+  for (int u = 0; u < T; ++u) {
     if (FLAGS && u >= f.count) continue;
     const bool pad = FLAGS && (f.pad >> u & 1), fresh = FLAGS && (f.fresh >> u & 1);
-    if (u % T == 0 && kept) {
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) kept[(long long)(u / T) * a.B * a.d + v] = h[v];
-    }
     float y[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
@@ -431,30 +386,41 @@ __device__ __forceinline__ void run_steps(const LruArgs& a, const Lane& n, int t
   }
 }
 
-// A workgroup's place in the scan.
-struct Place {
-  int rank, waves, wave, t0;
-};
-
-template <bool FLAGS, bool SERIES, bool BF16, int VEC, int N>
-__device__ __forceinline__ void lru_body(const LruArgs& a, const Chain& c, const Lane& n,
-                                         const Place& p, const Flags& f, const float (&k)[VEC],
-                                         const float (&first)[VEC], const Pack<BF16, VEC> (&x)[N],
-                                         const Pack<BF16, VEC> (&r)[N],
-                                         const Pack<BF16, VEC> (&i)[N], Map* maps, Map* win) {
-  float A[N][VEC], Bv[N][VEC], seg_in[VEC], h[VEC];
-  Map m[VEC];
-  step_maps<FLAGS, SERIES, BF16, VEC, N>(x, r, i, k, f, A, Bv, m);
+// A wave's way through its workgroup's segments: the loads of the next one are
+// under way from when this one's values have been used.
+template <bool FLAGS, bool SERIES, bool BF16, int VEC, int W>
+__device__ __forceinline__ void lru_walk(const LruArgs& a, const Lane& n, int rank, int last,
+                                         int wave, int waves, const float (&k)[VEC],
+                                         float (&seg_in)[VEC], Pack<BF16, VEC> (&x)[T],
+                                         Pack<BF16, VEC> (&r)[T],
+                                         Pack<BF16, VEC> (&i)[T], Marks marks,
+                                         Shared<VEC, W>& sh) {
+  int set = 0;
+#pragma unroll 1
+  for (; rank < last; ++rank, set ^= 1) {
+    const int t0 = (rank * waves + wave) * T;
+    const Flags f = flags_of<FLAGS>(a, t0, marks);
+    float A[T][VEC], Bv[T][VEC], h[VEC];
+    Map m[VEC];
+    step_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, k, f, A, Bv, m);
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) maps[(p.wave * VEC + v) * 64 + (threadIdx.x & 63)] = m[v];
-  __syncthreads();
-  join_segments<4>(c, a, n, p.rank, p.waves, maps, win, first, seg_in);
-  enter_wave<4>(maps, p.wave, seg_in, h);
-  if (!n.live || f.count == 0) return;
-  run_steps<FLAGS, BF16, VEC, N>(a, n, p.t0, f, A, Bv, h);
-  if (a.h_last && p.t0 + N >= a.L) {
+    for (int v = 0; v < VEC; ++v) sh.maps[set][(wave * VEC + v) * 64 + (threadIdx.x & 63)] = m[v];
+    if (rank + 1 < last) {
+      const int t1 = t0 + waves * T;
+      load_steps<BF16, VEC>(a, a.r, n, t1, r);
+      load_steps<BF16, VEC>(a, a.i, n, t1, i);
+      load_steps<BF16, VEC>(a, a.x, n, t1, x);
+      marks = load_marks<FLAGS>(a, n, t1);
+    }
+    __syncthreads();
+    enter_wave<4>(sh.maps[set], wave, waves, seg_in, h);
+    if (n.live && f.count) {
+      run_steps<FLAGS, BF16, VEC>(a, n, t0, f, A, Bv, h);
+      if (a.h_last && t0 + T >= a.L) {
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) a.h_last[n.chan + v] = h[v];
+        for (int v = 0; v < VEC; ++v) a.h_last[n.chan + v] = h[v];
+      }
+    }
   }
 }
 
@@ -462,31 +428,62 @@ __device__ __forceinline__ void lru_body(const LruArgs& a, const Chain& c, const
 // are missing.  All waves of a workgroup have the same channels, so all take
 // the same body.
 template <bool BF16, int VEC, bool FLAGS, int W>
-__global__ __launch_bounds__(64 * W, W == 16 ? 4 : 5) void lru_kernel(LruArgs a, Chain c) {
-  constexpr int N = kLruForward;
-  __shared__ Map maps[W * VEC * 64], win[kLook * VEC * 64];
-  __shared__ float rates[VEC * 64];
-  __shared__ unsigned ticket;
-  const int group = blockIdx.x % (unsigned)c.groups;
-  Place p;
-  p.rank = take_ticket(c, group, &ticket);
-  p.waves = blockDim.x >> 6;
-  p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  p.t0 = (p.rank * p.waves + p.wave) * N;
+__global__ __launch_bounds__(64 * W, 4) void lru_kernel(LruArgs a, Cut c) {
+  __shared__ Shared<VEC, W> sh;
+  const int group = blockIdx.x % (unsigned)c.groups, chunk = blockIdx.x / (unsigned)c.groups;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const Lane n = lane_of<VEC>(a, group);
-
-  Pack<BF16, VEC> x[N], r[N], i[N];
-  load_steps<BF16, VEC, N>(a, a.r, n, p.t0, r);
-  load_steps<BF16, VEC, N>(a, a.i, n, p.t0, i);
-  load_steps<BF16, VEC, N>(a, a.x, n, p.t0, x);
-  const Flags f = flags_of<FLAGS, N>(a, n, p.t0);
-  float k[VEC], first[VEC];
+  const int rank = chunk * c.each, last = min(rank + c.each, c.nseg);
+  const int t0 = (rank * waves + wave) * T;
+  Pack<BF16, VEC> x[T], r[T], i[T];
+  load_steps<BF16, VEC>(a, a.r, n, t0, r);
+  load_steps<BF16, VEC>(a, a.i, n, t0, i);
+  load_steps<BF16, VEC>(a, a.x, n, t0, x);
+  const Marks marks = load_marks<FLAGS>(a, n, t0);
+  float k[VEC], in[VEC];
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) first[v] = a.h0 && n.live ? a.h0[n.chan + v] : 0.f;
-  if (decay_rates<VEC>(a, c.rates, n, rates, k))
-    lru_body<FLAGS, true, BF16, VEC, N>(a, c, n, p, f, k, first, x, r, i, maps, win);
+  for (int v = 0; v < VEC; ++v) in[v] = a.h0 && n.live ? a.h0[n.chan + v] : 0.f;
+  enter_chunk(a, c, n, chunk, sh, in);
+  if (decay_rates<VEC>(a, n, sh.rates, k))
+    lru_walk<FLAGS, true, BF16, VEC, W>(a, n, rank, last, wave, waves, k, in, x, r, i, marks, sh);
   else
-    lru_body<FLAGS, false, BF16, VEC, N>(a, c, n, p, f, k, first, x, r, i, maps, win);
+    lru_walk<FLAGS, false, BF16, VEC, W>(a, n, rank, last, wave, waves, k, in, x, r, i, marks, sh);
+}
+
+// The maps of all chunks but the last: a wave has its steps in a row.
+template <bool FLAGS, bool SERIES, bool BF16, int VEC>
+__device__ __forceinline__ void run_map(const LruArgs& a, const Lane& n, int t0, int count,
+                                        const float (&k)[VEC], Map (&m)[VEC]) {
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) m[v] = Map{1.f, 0.f};
+#pragma unroll 1
+  for (int q = 0; q < count; ++q, t0 += T) {
+    Pack<BF16, VEC> x[T], r[T], i[T];
+    load_steps<BF16, VEC>(a, a.r, n, t0, r);
+    load_steps<BF16, VEC>(a, a.i, n, t0, i);
+    load_steps<BF16, VEC>(a, a.x, n, t0, x);
+    const Flags f = flags_of<FLAGS>(a, t0, load_marks<FLAGS>(a, n, t0));
+    float A[T][VEC], Bv[T][VEC];
+    Map one[VEC];
+    step_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, k, f, A, Bv, one);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) m[v] = join(one[v], m[v]);
+  }
+}
+template <bool BF16, int VEC, bool FLAGS, int W>
+__global__ __launch_bounds__(64 * W, 5) void lru_maps_kernel(LruArgs a, Cut c) {
+  __shared__ Shared<VEC, W> sh;
+  const int group = blockIdx.x % (unsigned)c.groups, chunk = blockIdx.x / (unsigned)c.groups;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Lane n = lane_of<VEC>(a, group);
+  const int t0 = (chunk * W + wave) * c.each * T;
+  float k[VEC];
+  Map m[VEC];
+  if (decay_rates<VEC>(a, n, sh.rates, k))
+    run_map<FLAGS, true, BF16, VEC>(a, n, t0, c.each, k, m);
+  else
+    run_map<FLAGS, false, BF16, VEC>(a, n, t0, c.each, k, m);
+  chunk_map(a, c, n, chunk, wave, sh, m);
 }
 
 // ------------------------------------------------------------------- gradient
@@ -576,83 +573,156 @@ __device__ __forceinline__ void grad_steps(const LruArgs& a, const Lane& n, int 
   }
 }
 
-template <bool FLAGS, bool SERIES, bool BF16, int VEC>
-__device__ __forceinline__ void grad_body(const LruArgs& a, const Chain& c, const Lane& n,
-                                          const Place& p, const Flags& f, const float (&k)[VEC],
-                                          const float (&first)[VEC], float (&h)[VEC],
-                                          const Pack<BF16, VEC> (&x)[T],
-                                          const Pack<BF16, VEC> (&r)[T],
-                                          const Pack<BF16, VEC> (&i)[T],
-                                          const Pack<BF16, VEC> (&dh)[T], Map* maps, Map* win,
-                                          float (&acc)[VEC]) {
-  GradSteps<VEC> st;
-  float seg_in[VEC], carry[VEC];
-  Map m[VEC];
-  grad_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, dh, k, f, h, st, m);
-  const int place = p.waves - 1 - p.wave;
+template <bool FLAGS, bool SERIES, bool BF16, int VEC, int W>
+__device__ __forceinline__ void grad_walk(const LruArgs& a, const Lane& n, int nseg, int rank,
+                                          int last, int wave, int waves, const float (&k)[VEC],
+                                          float (&seg_in)[VEC], float (&h)[VEC],
+                                          Pack<BF16, VEC> (&x)[T], Pack<BF16, VEC> (&r)[T],
+                                          Pack<BF16, VEC> (&i)[T], Pack<BF16, VEC> (&dh)[T],
+                                          Marks marks, Shared<VEC, W>& sh, float (&acc)[VEC]) {
+  const int place = waves - 1 - wave, lane = threadIdx.x & 63;
 #pragma unroll
-  for (int v = 0; v < VEC; ++v)
-    maps[(place * VEC + v) * 64 + (threadIdx.x & 63)] = f.count ? m[v] : Map{1.f, 0.f};
-  __syncthreads();
-  join_segments<1>(c, a, n, p.rank, p.waves, maps, win, first, seg_in);
-  enter_wave<1>(maps, place, seg_in, carry);
-  if (!n.live || f.count == 0) return;
-  grad_steps<FLAGS, BF16, VEC>(a, n, p.t0, dh, st, f, carry, acc);
-  if (a.dh0 && p.t0 == 0) {
+  for (int v = 0; v < VEC; ++v) acc[v] = 0.f;
+  int set = 0;
+#pragma unroll 1
+  for (; rank < last; ++rank, set ^= 1) {
+    const int t0 = ((nseg - 1 - rank) * waves + wave) * T;
+    const Flags f = flags_of<FLAGS>(a, t0, marks);
+    GradSteps<VEC> st;
+    Map m[VEC];
+    grad_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, dh, k, f, h, st, m);
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) a.dh0[n.chan + v] = carry[v];
+    for (int v = 0; v < VEC; ++v)
+      sh.maps[set][(place * VEC + v) * 64 + lane] = f.count ? m[v] : Map{1.f, 0.f};
+    Pack<BF16, VEC> now[T];
+#pragma unroll
+    for (int u = 0; u < T; ++u) now[u] = dh[u];
+    if (rank + 1 < last) {
+      const int t1 = t0 - waves * T;
+      load_steps<BF16, VEC>(a, a.r, n, t1, r);
+      load_steps<BF16, VEC>(a, a.dh, n, t1, dh);
+      load_steps<BF16, VEC>(a, a.i, n, t1, i);
+      load_steps<BF16, VEC>(a, a.x, n, t1, x);
+      marks = load_marks<FLAGS>(a, n, t1);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v)
+        h[v] = n.live ? a.states[(long long)(t1 / T) * a.B * a.d + n.chan + v] : 0.f;
+    }
+    __syncthreads();
+    float carry[VEC];
+    enter_wave<1>(sh.maps[set], place, waves, seg_in, carry);
+    if (n.live && f.count) {
+      grad_steps<FLAGS, BF16, VEC>(a, n, t0, now, st, f, carry, acc);
+      if (a.dh0 && t0 == 0) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) a.dh0[n.chan + v] = carry[v];
+      }
+    }
   }
 }
 
 // The scan runs from the last step to the first: rank 0 is the last segment,
-// and a workgroup's last wave comes first.  sums: [nseg, B, d] of -sum dla s.
+// and a workgroup's last wave comes first.  sums: [chunks, B, d] of -sum dla s.
 template <bool BF16, int VEC, bool FLAGS, int W>
-__global__ __launch_bounds__(64 * W, 3) void lru_grad_kernel(LruArgs a, Chain c, float* sums) {
-  __shared__ Map maps[W * VEC * 64], win[kLook * VEC * 64];
-  __shared__ float rates[VEC * 64];
-  __shared__ unsigned ticket;
-  const int group = blockIdx.x % (unsigned)c.groups;
-  Place p;
-  p.rank = take_ticket(c, group, &ticket);
-  p.waves = blockDim.x >> 6;
-  p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int seg = c.nseg - 1 - p.rank;
-  p.t0 = (seg * p.waves + p.wave) * T;
+__global__ __launch_bounds__(64 * W, 2) void lru_grad_kernel(LruArgs a, Cut c, float* sums) {
+  __shared__ Shared<VEC, W> sh;
+  const int group = blockIdx.x % (unsigned)c.groups, chunk = blockIdx.x / (unsigned)c.groups;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const Lane n = lane_of<VEC>(a, group);
-
+  const int rank = chunk * c.each, last = min(rank + c.each, c.nseg);
+  const int t0 = ((c.nseg - 1 - rank) * waves + wave) * T;
   Pack<BF16, VEC> x[T], r[T], i[T], dh[T];
-  load_steps<BF16, VEC, T>(a, a.r, n, p.t0, r);
-  load_steps<BF16, VEC, T>(a, a.dh, n, p.t0, dh);
-  load_steps<BF16, VEC, T>(a, a.i, n, p.t0, i);
-  load_steps<BF16, VEC, T>(a, a.x, n, p.t0, x);
-  const Flags f = flags_of<FLAGS, T>(a, n, p.t0);
-  float k[VEC], first[VEC], h[VEC], acc[VEC];
+  load_steps<BF16, VEC>(a, a.r, n, t0, r);
+  load_steps<BF16, VEC>(a, a.dh, n, t0, dh);
+  load_steps<BF16, VEC>(a, a.i, n, t0, i);
+  load_steps<BF16, VEC>(a, a.x, n, t0, x);
+  const Marks marks = load_marks<FLAGS>(a, n, t0);
+  float k[VEC], in[VEC], h[VEC], acc[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
-    first[v] = a.dh_last && n.live ? a.dh_last[n.chan + v] : 0.f;
-    h[v] = n.live && f.count ? a.states[(long long)(p.t0 / T) * a.B * a.d + n.chan + v] : 0.f;
-    acc[v] = 0.f;
+    in[v] = a.dh_last && n.live ? a.dh_last[n.chan + v] : 0.f;
+    h[v] = n.live && t0 < a.L ? a.states[(long long)(t0 / T) * a.B * a.d + n.chan + v] : 0.f;
   }
-  if (decay_rates<VEC>(a, c.rates, n, rates, k))
-    grad_body<FLAGS, true, BF16, VEC>(a, c, n, p, f, k, first, h, x, r, i, dh, maps, win, acc);
+  enter_chunk(a, c, n, chunk, sh, in);
+  if (decay_rates<VEC>(a, n, sh.rates, k))
+    grad_walk<FLAGS, true, BF16, VEC, W>(a, n, c.nseg, rank, last, wave, waves, k, in, h, x, r, i,
+                                         dh, marks, sh, acc);
   else
-    grad_body<FLAGS, false, BF16, VEC>(a, c, n, p, f, k, first, h, x, r, i, dh, maps, win, acc);
+    grad_walk<FLAGS, false, BF16, VEC, W>(a, n, c.nseg, rank, last, wave, waves, k, in, h, x, r, i,
+                                          dh, marks, sh, acc);
 
   // the waves' sums in a fixed order
-  float* red = reinterpret_cast<float*>(win);
+  float* red = reinterpret_cast<float*>(sh.maps);
   const int lane = threadIdx.x & 63;
   __syncthreads();
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) red[(p.wave * VEC + v) * 64 + lane] = acc[v];
+  for (int v = 0; v < VEC; ++v) red[(wave * VEC + v) * 64 + lane] = acc[v];
   __syncthreads();
-  if (p.wave == 0 && n.live) {
+  if (wave == 0 && n.live) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       float t = acc[v];
-      for (int q = 1; q < p.waves; ++q) t += red[(q * VEC + v) * 64 + lane];
-      sums[(long long)seg * a.B * a.d + n.chan + v] = t;
+      for (int q = 1; q < waves; ++q) t += red[(q * VEC + v) * 64 + lane];
+      sums[chunk * ((long long)a.B * a.d) + n.chan + v] = t;
     }
   }
+}
+
+// The maps of the carried gradient of all chunks but the last in the order of the
+// scan, by r and dh alone.
+template <bool FLAGS, bool SERIES, bool BF16, int VEC>
+__device__ __forceinline__ void grad_run_map(const LruArgs& a, const Lane& n, int t0, int count,
+                                             const float (&k)[VEC], Map (&m)[VEC]) {
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) m[v] = Map{1.f, 0.f};
+  t0 += (count - 1) * T;
+#pragma unroll 1
+  for (int q = 0; q < count; ++q, t0 -= T) {
+    Pack<BF16, VEC> r[T], dh[T];
+    load_steps<BF16, VEC>(a, a.r, n, t0, r);
+    load_steps<BF16, VEC>(a, a.dh, n, t0, dh);
+    const Flags f = flags_of<FLAGS>(a, t0, load_marks<FLAGS>(a, n, t0));
+    if (f.count == 0) continue;
+    Map one[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) one[v] = Map{1.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < T; ++u) {
+      const bool pad = FLAGS && ((f.pad >> u & 1) || u >= f.count);
+      const bool cut = FLAGS && (f.fresh & (2u << u) - 1) != 0;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const Decay dc = decay_of<SERIES>(decay_kept<SERIES>(k[v], sigmoid_fast(r[u].get(v))));
+        const float A = one[v].A * dc.a;
+        const float B = fmaf(A, dh[u].get(v), one[v].B);
+        one[v].A = pad ? one[v].A : A;
+        one[v].B = pad || cut ? one[v].B : B;
+      }
+    }
+    const bool anew = FLAGS && f.fresh != 0;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      one[v].A = anew ? 0.f : fmaxf(one[v].A, kTiny);
+      m[v] = join(one[v], m[v]);
+    }
+  }
+}
+template <bool BF16, int VEC, bool FLAGS, int W>
+__global__ __launch_bounds__(64 * W, 5) void lru_grad_maps_kernel(LruArgs a, Cut c) {
+  __shared__ Shared<VEC, W> sh;
+  const int group = blockIdx.x % (unsigned)c.groups, chunk = blockIdx.x / (unsigned)c.groups;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Lane n = lane_of<VEC>(a, group);
+  // the chunk's first segment in time
+  const int first = c.nseg - (chunk + 1) * c.each;
+  const int t0 = (first * W + wave * c.each) * T;
+  float k[VEC];
+  Map m[VEC];
+  if (decay_rates<VEC>(a, n, sh.rates, k))
+    grad_run_map<FLAGS, true, BF16, VEC>(a, n, t0, c.each, k, m);
+  else
+    grad_run_map<FLAGS, false, BF16, VEC>(a, n, t0, c.each, k, m);
+  chunk_map(a, c, n, chunk, W - 1 - wave, sh, m);
 }
 
 // dlam = c sigma(lam) sum over rows of [rows, d]: 64 features a workgroup, its
@@ -676,20 +746,42 @@ __global__ __launch_bounds__(1024) void lru_sums_kernel(LruArgs a, const float* 
   }
 }
 
-// Waves of a workgroup and segments of a sequence.  Small workgroups overlap
-// their loads with each other's arithmetic best; few channels make many segments
-// in a row, where what counts is how many hops a state takes: larger ones.
-int steps_of(bool grad) { return grad ? T : kLruForward; }
+// How a call is cut, by its groups of 64 channels of a sequence (us, bf16, forward
+// and gradient, one box):
+// - many: two channels a lane, small workgroups, which overlap each other's loads
+//   and arithmetic.  L 256, B 64, d 1024 (1,024 groups): 32 / 61; workgroups of 16
+//   and 8 waves of one channel a lane 44 / 70.
+// - fewer, or few steps: one channel a lane, so twice the workgroups, and large
+//   ones.  L 1024, B 16, d 1024 (256 groups): 38 / 65, as chunks 56 / 74; L 200,
+//   B 16, d 256: 11.7 / 19.2, as chunks 15.5 / 22.  L 256, B 32, d 1024 (512
+//   groups): the forward, whose small workgroups have eight waves, takes 19 with
+//   two channels a lane and 22 so; L 512, B 48, d 1024 the gradient 101 and 94.
+// - few groups, many steps: chunks, so many that there are about 512 workgroups of
+//   two channels a lane.  L 32768, B 1, d 1024 (16 groups): 110 / 143; as many
+//   chunks of one channel a lane 127 / 149; L 8192, B 8, d 1024 (128 groups): 206 /
+//   260, without chunks 236 / 359.
+constexpr long long kMany = 512, kGradMany = 1024, kFew = 256, kChunked = 1024, kMostChunks = 256;
+constexpr int kWideRounds = 4;
 struct Plan {
-  int full, waves, nseg;
+  bool wide;                      // large workgroups of one channel a lane
+  int waves, nseg, each, chunks;  // of a workgroup, segments, those of a chunk, chunks
 };
 Plan plan(int L, int B, int d, bool grad) {
-  const int n = (L + steps_of(grad) - 1) / steps_of(grad);
-  const bool few = (long long)B * d < kFewChannels;
+  const int n = (L + T - 1) / T;
+  const long long groups = (long long)B * ((d + 63) / 64);
+  const int wide = grad ? kWideGradWaves : kWideWaves;
   Plan p;
-  p.full = grad ? (few ? 12 : 4) : (few ? 16 : 8);
-  p.waves = std::min(n, p.full);
-  p.nseg = (n + p.full - 1) / p.full;
+  p.wide = groups < (grad ? kGradMany : kMany) && (groups >= kFew || n <= kWideRounds * wide);
+  const int most = p.wide ? wide : grad ? kGradWaves : kWaves;
+  p.nseg = (n + most - 1) / most;
+  p.waves = (n + p.nseg - 1) / p.nseg;
+  p.each = p.nseg, p.chunks = 1;
+  if (!p.wide && groups < kFew) {
+    const long long want = std::min({(kChunked + groups - 1) / groups, (long long)p.nseg, kMostChunks});
+    p.waves = most;
+    p.each = (int)((p.nseg + want - 1) / want);
+    p.chunks = (p.nseg + p.each - 1) / p.each;
+  }
   return p;
 }
 
@@ -706,88 +798,80 @@ bool pairs_ok(const LruArgs& a, F each) {
 }
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
-// Workspace of several segments: words (an even number), tickets (of as many
-// workgroups as one channel a lane makes), rates.
-struct Layout {
-  size_t words, tickets, rates, total;
-};
-Layout layout(int L, int B, int d, bool grad) {
-  const int nseg = plan(L, B, d, grad).nseg;
-  const size_t lanes = (size_t)B * d, groups = (size_t)B * ((d + 63) / 64);
-  Layout l;
-  l.words = sizeof(unsigned long long) * ((nseg * lanes + 1) / 2 * 2);
-  l.tickets = align_up(l.words);
-  l.rates = l.tickets + align_up(sizeof(unsigned) * kTicketPitch * groups);
-  l.total = nseg == 1 ? 0 : l.rates + align_up(sizeof(float) * d);
-  return l;
-}
-
-hipError_t clear(const Chain& c, const LruArgs& a, hipStream_t st) {
-  const long long pairs = ((long long)c.nseg * a.B * a.d + 1) / 2;
-  const long long most = std::max({pairs, (long long)c.groups * kTicketPitch, (long long)a.d});
-  const long long blocks = (most + 511) / 512;
-  timing_before("lru_clear", st);
-  hipLaunchKernelGGL(lru_clear_kernel, dim3((unsigned)std::min(blocks, 2048LL)), dim3(256), 0, st,
-                     a, c, pairs);
-  timing_after(st);
-  return hipGetLastError();
-}
-
-template <bool BF16, int VEC, bool FLAGS>
-void launch(const LruArgs& a, const Chain& c, const Plan& p, float* sums, bool grad,
-            hipStream_t st) {
-  const dim3 grid((unsigned)c.groups * p.nseg), block(64 * p.waves);
-  if (grad && p.full == 4)
-    hipLaunchKernelGGL((lru_grad_kernel<BF16, VEC, FLAGS, 4>), grid, block, 0, st, a, c, sums);
-  else if (grad)
-    hipLaunchKernelGGL((lru_grad_kernel<BF16, VEC, FLAGS, 12>), grid, block, 0, st, a, c, sums);
-  else if (p.full == 8)
-    hipLaunchKernelGGL((lru_kernel<BF16, VEC, FLAGS, 8>), grid, block, 0, st, a, c);
-  else
-    hipLaunchKernelGGL((lru_kernel<BF16, VEC, FLAGS, 16>), grid, block, 0, st, a, c);
-}
-
-template <bool BF16, int VEC>
-hipError_t run(const LruArgs& a, bool grad, hipStream_t st) {
-  const Plan p = plan(a.L, a.B, a.d, grad);
-  Chain c{};
-  c.nseg = p.nseg;
-  c.groups = a.B * ((a.d + 64 * VEC - 1) / (64 * VEC));
-  char* ws = static_cast<char*>(a.workspace);
-  const Layout l = layout(a.L, a.B, a.d, grad);
-  if (p.nseg > 1) {
-    c.words = reinterpret_cast<unsigned long long*>(ws);
-    c.tickets = reinterpret_cast<unsigned*>(ws + l.tickets);
-    c.rates = reinterpret_cast<float*>(ws + l.rates);
-    if (hipError_t e = clear(c, a, st)) return e;
+template <bool BF16, int VEC, bool FLAGS, bool WIDE>
+void launch(const LruArgs& a, const Cut& c, const Plan& p, hipStream_t st) {
+  constexpr int W = WIDE ? kWideWaves : kWaves;
+  if constexpr (!WIDE) {
+    if (c.chunks > 1) {
+      timing_before("lru_maps", st);
+      hipLaunchKernelGGL((lru_maps_kernel<BF16, VEC, FLAGS, W>),
+                         dim3((unsigned)c.groups * (c.chunks - 1)), dim3(64 * W), 0, st, a, c);
+      timing_after(st);
+    }
   }
-  float* sums = reinterpret_cast<float*>(ws + l.total);
-  timing_before(grad ? "lru_grad" : "lru", st);
-  if (a.mask || a.reset || a.L % steps_of(grad))
-    launch<BF16, VEC, true>(a, c, p, sums, grad, st);
-  else
-    launch<BF16, VEC, false>(a, c, p, sums, grad, st);
+  timing_before("lru", st);
+  hipLaunchKernelGGL((lru_kernel<BF16, VEC, FLAGS, W>), dim3((unsigned)c.groups * c.chunks),
+                     dim3(64 * p.waves), 0, st, a, c);
   timing_after(st);
-  if (hipError_t e = hipGetLastError()) return e;
-  if (!grad) return hipSuccess;
+}
+template <bool BF16, int VEC, bool FLAGS, bool WIDE>
+void launch_grad(const LruArgs& a, const Cut& c, const Plan& p, float* sums, hipStream_t st) {
+  constexpr int W = WIDE ? kWideGradWaves : kGradWaves;
+  if constexpr (!WIDE) {
+    if (c.chunks > 1) {
+      timing_before("lru_grad_maps", st);
+      hipLaunchKernelGGL((lru_grad_maps_kernel<BF16, VEC, FLAGS, W>),
+                         dim3((unsigned)c.groups * (c.chunks - 1)), dim3(64 * W), 0, st, a, c);
+      timing_after(st);
+    }
+  }
+  timing_before("lru_grad", st);
+  hipLaunchKernelGGL((lru_grad_kernel<BF16, VEC, FLAGS, W>), dim3((unsigned)c.groups * c.chunks),
+                     dim3(64 * p.waves), 0, st, a, c, sums);
+  timing_after(st);
   timing_before("lru_sums", st);
   hipLaunchKernelGGL(lru_sums_kernel, dim3((a.d + 63) / 64), dim3(1024), 0, st, a, sums,
-                     (long long)p.nseg * a.B);
+                     (long long)c.chunks * a.B);
   timing_after(st);
+}
+
+// Workspace: the chunks' maps, then (gradient) the sums.
+size_t maps_bytes(const Plan& p, int B, int d) {
+  return align_up(sizeof(Map) * (size_t)(p.chunks - 1) * B * d);
+}
+
+template <bool BF16, int VEC, bool WIDE>
+hipError_t run(const LruArgs& a, const Plan& p, bool grad, hipStream_t st) {
+  const Cut c{static_cast<Map*>(a.workspace), p.nseg, p.each, p.chunks,
+              a.B * ((a.d + 64 * VEC - 1) / (64 * VEC))};
+  float* sums = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + maps_bytes(p, a.B, a.d));
+  const bool flags = a.mask || a.reset || a.L % T;
+  if (grad && flags)
+    launch_grad<BF16, VEC, true, WIDE>(a, c, p, sums, st);
+  else if (grad)
+    launch_grad<BF16, VEC, false, WIDE>(a, c, p, sums, st);
+  else if (flags)
+    launch<BF16, VEC, true, WIDE>(a, c, p, st);
+  else
+    launch<BF16, VEC, false, WIDE>(a, c, p, st);
   return hipGetLastError();
 }
 
 hipError_t dispatch(const LruArgs& a, bool grad, bool pairs, hipStream_t st) {
-  if (a.bf16) return pairs ? run<true, 2>(a, grad, st) : run<true, 1>(a, grad, st);
-  return pairs && !grad ? run<false, 2>(a, grad, st) : run<false, 1>(a, grad, st);
+  const Plan p = plan(a.L, a.B, a.d, grad);
+  if (!a.bf16)
+    return p.wide ? run<false, 1, true>(a, p, grad, st) : run<false, 1, false>(a, p, grad, st);
+  if (p.wide) return run<true, 1, true>(a, p, grad, st);
+  return pairs ? run<true, 2, false>(a, p, grad, st) : run<true, 1, false>(a, p, grad, st);
 }
 
 }  // namespace
 
-size_t lru_workspace_bytes(int L, int B, int d) { return layout(L, B, d, false).total; }
+size_t lru_workspace_bytes(int L, int B, int d) { return maps_bytes(plan(L, B, d, false), B, d); }
 
 size_t lru_grad_workspace_bytes(int L, int B, int d) {
-  return layout(L, B, d, true).total + sizeof(float) * (size_t)plan(L, B, d, true).nseg * B * d;
+  const Plan p = plan(L, B, d, true);
+  return maps_bytes(p, B, d) + sizeof(float) * (size_t)p.chunks * B * d;
 }
 
 long long lru_blocks(int L, int B, int d) {

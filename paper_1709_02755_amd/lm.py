@@ -73,6 +73,11 @@ def _out(out, name, shape, dtype, like):
     return t
 
 
+def _new_like(like):
+    """A new contiguous tensor of the shape and type of `like`."""
+    return torch.empty_like(like) if like.is_contiguous() else like.new_empty(like.shape)
+
+
 def _logits(logits, temperature):
     """(code, N, V, device, pitch) of checked logits."""
     code = _dtype(logits, "logits")
@@ -88,7 +93,7 @@ def _logits(logits, temperature):
 def _dlogits(dlogits, logits, dv):
     """(dlogits, its pitch): the caller's, which may be the logits, or new."""
     if dlogits is None:
-        dlogits = logits.new_empty(logits.shape)
+        dlogits = _new_like(logits)
     return dlogits, _pitch(dlogits, "dlogits", logits.shape, logits.dtype, dv)
 
 
@@ -280,7 +285,7 @@ def _row_out(out, name, like):
     pitch)."""
     t = None if out is None else out.get(name)
     if t is None:
-        return like.new_empty(like.shape), like.shape[-1]
+        return _new_like(like), like.shape[-1]
     return t, _row_pitch(t, name, like.shape, like.dtype, like.device)
 
 
@@ -381,7 +386,7 @@ def _seq_out(out, name, like):
     t = None if out is None else out.get(name)
     if t is None:
         _, B, d = like.shape
-        return like.new_empty(like.shape), (B * d, d)
+        return _new_like(like), (B * d, d)
     return t, _seq(t, name, like.shape, like.dtype, like.device)
 
 
@@ -466,7 +471,7 @@ def lru_step(x, r, i, lam, h, c=8.0, out=None, mask=None, reset=None):
     _req(mask, "mask", (B,), dtype=torch.uint8, optional=True, device=dv)
     _req(reset, "reset", (B,), dtype=torch.uint8, optional=True, device=dv)
     if out is None:
-        out, so = x.new_empty(shape), d
+        out, so = _new_like(x), d
     else:
         so = _step_rows(out, "out", shape, dt, dv)
     hp = _ptr(h)

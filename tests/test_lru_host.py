@@ -14,7 +14,7 @@ FAKE = ctypes.c_void_p(0x10000)
 ODD = ctypes.c_void_p(0x10001)
 HALF = ctypes.c_void_p(0x10002)
 B16 = torch.bfloat16
-L, B, D = 200, 2, 8
+L, B, D = 1000, 2, 8
 
 
 def forward(**kw):
