@@ -14,7 +14,7 @@ from __future__ import annotations
 import torch
 
 from . import sru
-from .sru import _check, _ptr, _req, _ws
+from .sru import _check, _req, _ws
 
 DTYPE_FP32, DTYPE_BF16 = 0, 1
 MAX_TOP, MAX_TEACHER = 64, 1024
@@ -22,6 +22,21 @@ GATE_SILU, GATE_SIGMOID = 0, 1
 LRU_STEPS = 8
 
 _CODES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+
+
+_Tensor = torch.Tensor
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _plain(t, shape, dtype, device):
+    """Whether t is a contiguous tensor of this kind on a GPU device (one known
+    to be so): most arguments pass by this one expression, the others go to the
+    checks that name what is wrong.  A small call is bound by the host."""
+    return (t.__class__ is _Tensor and t.dtype is dtype and t.shape == shape
+            and t.device == device and t.is_contiguous())
 
 
 def _dtype(t, name):
@@ -64,12 +79,20 @@ def _pitch(t, name, shape, dtype, device):
 
 def _out(out, name, shape, dtype, like):
     """out[name] if the caller gave it (checked), else a new tensor on the
-    device of `like` (whose method makes it at half the cost of torch.empty: a
-    small call is bound by the host)."""
+    device of `like`."""
     t = None if out is None else out.get(name)
     if t is None:
         return like.new_empty(shape, dtype=dtype)
     _req(t, name, shape, dtype=dtype, device=like.device)
+    return t
+
+
+def _out_like(out, name, like):
+    """_out for one of the shape and type of the contiguous tensor `like`."""
+    t = None if out is None else out.get(name)
+    if t is None:
+        return torch.empty_like(like)
+    _req(t, name, like.shape, dtype=like.dtype, device=like.device)
     return t
 
 
@@ -229,7 +252,7 @@ def _row_pitch(t, name, shape, dtype, device):
     """The distance of consecutive rows of a [..., d] tensor (None: 0)."""
     if t is None:
         return 0
-    if t.__class__ is torch.Tensor and sru._fits(t, shape, dtype, device):
+    if _plain(t, shape, dtype, device):
         return shape[-1]
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a torch tensor")
@@ -276,7 +299,8 @@ def _norm_inputs(x, y, z, w_post, scale, w_pre):
     pitch = (_row_pitch(x, "x", shape, x.dtype, dv), _row_pitch(y, "y", shape, act, dv),
              _row_pitch(z, "z", shape, act, dv))
     for n, w in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
-        _req(w, n, (d,), optional=True, device=dv)
+        if w is not None and not _plain(w, (d,), _F32, dv):
+            _req(w, n, (d,), device=dv)
     return x.numel() // d if d else 0, d, act, code, res, dv, pitch
 
 
@@ -308,7 +332,7 @@ def residual_norm_forward(x, y=None, w_post=None, z=None, scale=None, w_pre=None
         x_out, ldxo = _row_out(out, "x_out", x)
     if w_pre is not None:
         o, ldo = _row_out(out, "o", x if y is None else y)
-    rstd = _out(out, "rstd", x.shape[:-1] + (2,), _F32, x)
+    rstd = _out(out, "rstd", (*x.shape[:-1], 2), _F32, x)
     st = sru.lib().sru_residual_norm_forward(M, d, code, res, gate, eps, _ptr(x), ldx, _ptr(y),
                                              ldy, _ptr(z), ldz, _ptr(w_post), _ptr(scale),
                                              _ptr(w_pre), _ptr(x_out), ldxo, _ptr(o), ldo,
@@ -333,7 +357,7 @@ def residual_norm_backward(x, y, rstd, dx_out=None, do=None, w_post=None, z=None
     g["dy"], lddy = _row_out(out, "dy", y) if y is not None else (None, 0)
     g["dz"], lddz = _row_out(out, "dz", z) if z is not None else (None, 0)
     for n, w in (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre)):
-        g[n] = None if w is None else _out(out, n, (d,), _F32, x)
+        g[n] = None if w is None else _out_like(out, n, w)
     lib = sru.lib()
     ws, nbytes = _ws(ws, lib.sru_residual_norm_backward_workspace_bytes(M, d), dv)
     st = lib.sru_residual_norm_backward(
@@ -375,8 +399,10 @@ def _lru_inputs(x, r, i, lam, mask, reset):
     steps = (_seq(x, "x", shape, x.dtype, dv), _seq(r, "r", shape, x.dtype, dv),
              _seq(i, "i", shape, x.dtype, dv))
     _req(lam, "lam", (d,), device=dv)
-    _req(mask, "mask", (L, B), dtype=torch.uint8, optional=True, device=dv)
-    _req(reset, "reset", (L, B), dtype=torch.uint8, optional=True, device=dv)
+    if mask is not None:
+        _req(mask, "mask", (L, B), dtype=torch.uint8, device=dv)
+    if reset is not None:
+        _req(reset, "reset", (L, B), dtype=torch.uint8, device=dv)
     return shape, code, dv, steps
 
 
@@ -430,7 +456,7 @@ def lru_backward(x, r, i, lam, states, dH, dh_last=None, mask=None, reset=None, 
     dx, sdx = _seq_out(out, "dx", x)
     dr, sdr = _seq_out(out, "dr", x)
     di, sdi = _seq_out(out, "di", x)
-    dlam = _out(out, "dlam", (d,), _F32, x)
+    dlam = _out_like(out, "dlam", lam)
     dh0 = _out(out, "dh0", (B, d), _F32, x) if want_dh0 else None
     lib = sru.lib()
     ws, nbytes = _ws(ws, lib.sru_lru_backward_workspace_bytes(L, B, d), dv)
@@ -466,10 +492,13 @@ def lru_step(x, r, i, lam, h, c=8.0, out=None, mask=None, reset=None):
     if not fast:  # one by one, for the message
         for n, t in (("x", x), ("r", r), ("i", i)):
             _step_rows(t, n, shape, dt, dv)
-    _req(lam, "lam", (d,), device=dv)
-    _req(h, "h", (B, d), device=dv)
-    _req(mask, "mask", (B,), dtype=torch.uint8, optional=True, device=dv)
-    _req(reset, "reset", (B,), dtype=torch.uint8, optional=True, device=dv)
+    if not (_plain(lam, (d,), _F32, dv) and _plain(h, shape, _F32, dv)):
+        _req(lam, "lam", (d,), device=dv)
+        _req(h, "h", (B, d), device=dv)
+    if mask is not None:
+        _req(mask, "mask", (B,), dtype=torch.uint8, device=dv)
+    if reset is not None:
+        _req(reset, "reset", (B,), dtype=torch.uint8, device=dv)
     if out is None:
         out, so = _new_like(x), d
     else:

@@ -118,7 +118,7 @@ def test_binding(stub):
     y = lm.lru_step(U[0, :, 0], U[0, :, 1], U[0, :, 2], lam, h)
     a = stub.calls[-1][1]
     assert y.shape == (B, d) and a[0:3] == (1, B, d) and a[6] == 3 * d
-    assert a[15].value == a[21].value == h.data_ptr()     # the state, in place
+    assert a[15] == a[21] == h.data_ptr()     # the state, in place
     reached = len(stub.calls)
     st = fw["states"]
     bad = [
