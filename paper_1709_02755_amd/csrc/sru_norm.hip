@@ -263,12 +263,14 @@ struct GradRow {
 
 // When a row's tensors are loaded.  Rows of up to a wave: all at once, in front
 // (2 or 3 waves run on a SIMD then, fewer than with loads where they are used,
-// but with more in flight: 16384 x 1024 bf16 beside fp32 104 -> 89 us, 65536 x
-// 256 145 -> 85).  256 threads to a row, which wait for each other twice a row:
+// but with more in flight: 16384 x 1024 bf16 beside fp32 104 -> 91 us, 65536 x
+// 256 145 -> 85; left to itself, the compiler takes registers past what 2 waves
+// can have, and 1 takes 109 us).  256 threads to a row, which wait for each other twice a row:
 // while the row before is worked on (8192 x 2048 121 -> 97 us).  Wider rows: each
 // where it is used (4096 x 4096 98 us, 105 in front).
 template <class H, bool ABF, bool RBF>
-__global__ __launch_bounds__(H::THREADS) void norm_grad_kernel(NormArgs a) {
+__global__ __launch_bounds__(H::THREADS, H::LANES > 64 ? 1 : H::F == 16 ? 2 : 3) void
+norm_grad_kernel(NormArgs a) {
   constexpr bool AHEAD = H::LANES == 256, WHOLE = AHEAD || H::NW == 1;
   __shared__ float lds[H::NW];
   __shared__ float sums[H::ROWS > 1 ? H::THREADS * H::F : 1];
