@@ -196,6 +196,17 @@ __device__ __forceinline__ Flags flags_of(const LruArgs& a, int t0, const Marks&
   return f;
 }
 
+// Most waves of a call with marks have none of their own, or only padding: they
+// take shorter ways (and the same values).
+template <bool FLAGS>
+__device__ __forceinline__ bool unmarked(const Flags& f) {
+  return !FLAGS || (f.count == T && (f.pad | f.fresh) == 0);
+}
+template <bool FLAGS>
+__device__ __forceinline__ bool all_padded(const Flags& f) {
+  return FLAGS && f.pad == (1u << f.count) - 1;
+}
+
 // A step's decay a = e^-y and q = 1 - a^2 from y = k s.  Both come from w = 1 -
 // a, by the series of 1 - e^-y where that would cancel (its next term is y^5 /
 // 720, below 2^-25 of w here): q = w (2 - w), and a = 1 - w is rounded once, to
@@ -379,8 +390,9 @@ __device__ __forceinline__ void run_steps(const LruArgs& a, const Lane& n, int t
     float y[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      h[v] = fresh ? Bv[u][v] : fmaf(A[u][v], h[v], Bv[u][v]);
-      y[v] = pad ? 0.f : h[v];
+      const float hn = fresh ? Bv[u][v] : fmaf(A[u][v], h[v], Bv[u][v]);
+      h[v] = pad ? h[v] : hn;
+      y[v] = pad ? 0.f : hn;
     }
     out.store(u, y);
   }
@@ -402,7 +414,14 @@ __device__ __forceinline__ void lru_walk(const LruArgs& a, const Lane& n, int ra
     const Flags f = flags_of<FLAGS>(a, t0, marks);
     float A[T][VEC], Bv[T][VEC], h[VEC];
     Map m[VEC];
-    step_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, k, f, A, Bv, m);
+    if (unmarked<FLAGS>(f)) {
+      step_maps<false, SERIES, BF16, VEC>(x, r, i, k, f, A, Bv, m);
+    } else if (all_padded<FLAGS>(f)) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) m[v] = Map{1.f, 0.f};
+    } else {
+      step_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, k, f, A, Bv, m);
+    }
 #pragma unroll
     for (int v = 0; v < VEC; ++v) sh.maps[set][(wave * VEC + v) * 64 + (threadIdx.x & 63)] = m[v];
     if (rank + 1 < last) {
@@ -415,7 +434,10 @@ __device__ __forceinline__ void lru_walk(const LruArgs& a, const Lane& n, int ra
     __syncthreads();
     enter_wave<4>(sh.maps[set], wave, waves, seg_in, h);
     if (n.live && f.count) {
-      run_steps<FLAGS, BF16, VEC>(a, n, t0, f, A, Bv, h);
+      if (unmarked<FLAGS>(f))
+        run_steps<false, BF16, VEC>(a, n, t0, f, A, Bv, h);
+      else
+        run_steps<FLAGS, BF16, VEC>(a, n, t0, f, A, Bv, h);
       if (a.h_last && t0 + T >= a.L) {
 #pragma unroll
         for (int v = 0; v < VEC; ++v) a.h_last[n.chan + v] = h[v];
@@ -463,9 +485,13 @@ __device__ __forceinline__ void run_map(const LruArgs& a, const Lane& n, int t0,
     load_steps<BF16, VEC>(a, a.i, n, t0, i);
     load_steps<BF16, VEC>(a, a.x, n, t0, x);
     const Flags f = flags_of<FLAGS>(a, t0, load_marks<FLAGS>(a, n, t0));
+    if (all_padded<FLAGS>(f)) continue;
     float A[T][VEC], Bv[T][VEC];
     Map one[VEC];
-    step_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, k, f, A, Bv, one);
+    if (unmarked<FLAGS>(f))
+      step_maps<false, SERIES, BF16, VEC>(x, r, i, k, f, A, Bv, one);
+    else
+      step_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, k, f, A, Bv, one);
 #pragma unroll
     for (int v = 0; v < VEC; ++v) m[v] = join(one[v], m[v]);
   }
@@ -590,10 +616,16 @@ __device__ __forceinline__ void grad_walk(const LruArgs& a, const Lane& n, int n
     const Flags f = flags_of<FLAGS>(a, t0, marks);
     GradSteps<VEC> st;
     Map m[VEC];
-    grad_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, dh, k, f, h, st, m);
+    if (all_padded<true>(f)) {  // or without a step
 #pragma unroll
-    for (int v = 0; v < VEC; ++v)
-      sh.maps[set][(place * VEC + v) * 64 + lane] = f.count ? m[v] : Map{1.f, 0.f};
+      for (int v = 0; v < VEC; ++v) m[v] = Map{1.f, 0.f};
+    } else if (unmarked<FLAGS>(f)) {
+      grad_maps<false, SERIES, BF16, VEC>(x, r, i, dh, k, f, h, st, m);
+    } else {
+      grad_maps<FLAGS, SERIES, BF16, VEC>(x, r, i, dh, k, f, h, st, m);
+    }
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) sh.maps[set][(place * VEC + v) * 64 + lane] = m[v];
     Pack<BF16, VEC> now[T];
 #pragma unroll
     for (int u = 0; u < T; ++u) now[u] = dh[u];
@@ -612,7 +644,10 @@ __device__ __forceinline__ void grad_walk(const LruArgs& a, const Lane& n, int n
     float carry[VEC];
     enter_wave<1>(sh.maps[set], place, waves, seg_in, carry);
     if (n.live && f.count) {
-      grad_steps<FLAGS, BF16, VEC>(a, n, t0, now, st, f, carry, acc);
+      if (unmarked<FLAGS>(f))
+        grad_steps<false, BF16, VEC>(a, n, t0, now, st, f, carry, acc);
+      else
+        grad_steps<FLAGS, BF16, VEC>(a, n, t0, now, st, f, carry, acc);
       if (a.dh0 && t0 == 0) {
 #pragma unroll
         for (int v = 0; v < VEC; ++v) a.dh0[n.chan + v] = carry[v];
@@ -624,7 +659,7 @@ __device__ __forceinline__ void grad_walk(const LruArgs& a, const Lane& n, int n
 // The scan runs from the last step to the first: rank 0 is the last segment,
 // and a workgroup's last wave comes first.  sums: [chunks, B, d] of -sum dla s.
 template <bool BF16, int VEC, bool FLAGS, int W>
-__global__ __launch_bounds__(64 * W, 2) void lru_grad_kernel(LruArgs a, Cut c, float* sums) {
+__global__ __launch_bounds__(64 * W, VEC == 1 ? 3 : 2) void lru_grad_kernel(LruArgs a, Cut c, float* sums) {
   __shared__ Shared<VEC, W> sh;
   const int group = blockIdx.x % (unsigned)c.groups, chunk = blockIdx.x / (unsigned)c.groups;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -668,6 +703,31 @@ __global__ __launch_bounds__(64 * W, 2) void lru_grad_kernel(LruArgs a, Cut c, f
   }
 }
 
+// The map of grad_maps alone.
+template <bool FLAGS, bool SERIES, bool BF16, int VEC>
+__device__ __forceinline__ void grad_map(const Pack<BF16, VEC> (&r)[T],
+                                         const Pack<BF16, VEC> (&dh)[T], const float (&k)[VEC],
+                                         const Flags& f, Map (&all)[VEC]) {
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) all[v] = Map{1.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < T; ++u) {
+    const bool pad = FLAGS && ((f.pad >> u & 1) || u >= f.count);
+    const bool cut = FLAGS && (f.fresh & (2u << u) - 1) != 0;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const Decay dc = decay_of<SERIES>(decay_kept<SERIES>(k[v], sigmoid_fast(r[u].get(v))));
+      const float A = all[v].A * dc.a;
+      const float B = fmaf(A, dh[u].get(v), all[v].B);
+      all[v].A = pad ? all[v].A : A;
+      all[v].B = pad || cut ? all[v].B : B;
+    }
+  }
+  const bool anew = FLAGS && f.fresh != 0;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) all[v].A = anew ? 0.f : fmaxf(all[v].A, kTiny);
+}
+
 // The maps of the carried gradient of all chunks but the last in the order of the
 // scan, by r and dh alone.
 template <bool FLAGS, bool SERIES, bool BF16, int VEC>
@@ -682,29 +742,14 @@ __device__ __forceinline__ void grad_run_map(const LruArgs& a, const Lane& n, in
     load_steps<BF16, VEC>(a, a.r, n, t0, r);
     load_steps<BF16, VEC>(a, a.dh, n, t0, dh);
     const Flags f = flags_of<FLAGS>(a, t0, load_marks<FLAGS>(a, n, t0));
-    if (f.count == 0) continue;
+    if (all_padded<true>(f)) continue;  // or without a step
     Map one[VEC];
+    if (unmarked<FLAGS>(f))
+      grad_map<false, SERIES, BF16, VEC>(r, dh, k, f, one);
+    else
+      grad_map<FLAGS, SERIES, BF16, VEC>(r, dh, k, f, one);
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) one[v] = Map{1.f, 0.f};
-#pragma unroll
-    for (int u = 0; u < T; ++u) {
-      const bool pad = FLAGS && ((f.pad >> u & 1) || u >= f.count);
-      const bool cut = FLAGS && (f.fresh & (2u << u) - 1) != 0;
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        const Decay dc = decay_of<SERIES>(decay_kept<SERIES>(k[v], sigmoid_fast(r[u].get(v))));
-        const float A = one[v].A * dc.a;
-        const float B = fmaf(A, dh[u].get(v), one[v].B);
-        one[v].A = pad ? one[v].A : A;
-        one[v].B = pad || cut ? one[v].B : B;
-      }
-    }
-    const bool anew = FLAGS && f.fresh != 0;
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      one[v].A = anew ? 0.f : fmaxf(one[v].A, kTiny);
-      m[v] = join(one[v], m[v]);
-    }
+    for (int v = 0; v < VEC; ++v) m[v] = join(one[v], m[v]);
   }
 }
 template <bool BF16, int VEC, bool FLAGS, int W>
