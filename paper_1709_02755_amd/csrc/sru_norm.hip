@@ -271,7 +271,7 @@ struct GradRow {
 // while the row before is worked on (8192 x 2048 121 -> 97 us).  Wider rows: each
 // where it is used (4096 x 4096 98 us, 105 in front).
 template <class H, bool ABF, bool RBF>
-__global__ __launch_bounds__(H::THREADS, H::LANES > 64 ? 1 : H::F == 16 ? 2 : 3) void
+__global__ __launch_bounds__(H::THREADS, H::LANES > 256 ? 1 : H::F == 16 ? 2 : 3) void
 norm_grad_kernel(NormArgs a) {
   constexpr bool AHEAD = H::LANES == 256, WHOLE = AHEAD || H::NW == 1;
   __shared__ float lds[H::NW];
@@ -441,21 +441,22 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(NormArgs a, int rows) {
 }
 
 // Workgroups of the gradient: each leaves one row of sums, so only as many as
-// run at a time (by the registers they take).
+// run at a time (by the registers they take; 8192 x 2048 with 512 of them 105 us, 96).
 int rows_at_once(int d) { return d <= 128 ? 16 : d <= 256 ? 8 : d <= 1024 ? 4 : 1; }
 int grad_blocks(int M, int d) {
-  const int most = d <= 512 ? 768 : d <= 4096 ? 512 : 256;
+  const int most = d <= 512 || (d > 1024 && d <= 2048) ? 768 : d <= 4096 ? 512 : 256;
   const int want = (int)(((long long)M + rows_at_once(d) - 1) / rows_at_once(d));
   return want < most ? want : most;
 }
 
-template <class H, bool ABF, bool RBF>
+// H: a row's threads and columns in the forward, G: in the gradient.
+template <bool ABF, bool RBF, class H, class G = H>
 hipError_t launch(const NormArgs& a, bool grad, hipStream_t st) {
   if (grad) {
-    static_assert(H::F == 8 || H::F == 16, "columns of a thread");
+    static_assert(G::F == 8 || G::F == 16, "columns of a thread");
     const int blocks = grad_blocks(a.M, a.d);
     timing_before("norm_grad", st);
-    hipLaunchKernelGGL((norm_grad_kernel<H, ABF, RBF>), dim3(blocks), dim3(H::THREADS), 0, st, a);
+    hipLaunchKernelGGL((norm_grad_kernel<G, ABF, RBF>), dim3(blocks), dim3(G::THREADS), 0, st, a);
     timing_after(st);
     if (hipError_t e = hipGetLastError()) return e;
     if (!a.dw_post && !a.dscale && !a.dw_pre) return hipSuccess;
@@ -476,17 +477,20 @@ hipError_t launch(const NormArgs& a, bool grad, hipStream_t st) {
 
 // Threads a row and columns a thread by the width: a row's columns stay in
 // registers, 8 to a thread (16 up to 1024 columns, where one wave then holds a
-// row and needs no barrier, and past 8192).
+// row and needs no barrier, and past 8192; past 4096 in the forward, which has
+// registers to spare and waits for fewer waves then: 2000 x 6000 fp32 60 -> 50 us,
+// while the gradient takes 97 with 8 and 103 with 16).
 template <int VE, bool ABF, bool RBF>
 hipError_t by_width(const NormArgs& a, bool grad, hipStream_t st) {
-  if (a.d <= 128) return launch<Hold<VE, 8 / VE, 16>, ABF, RBF>(a, grad, st);
-  if (a.d <= 256) return launch<Hold<VE, 8 / VE, 32>, ABF, RBF>(a, grad, st);
-  if (a.d <= 512) return launch<Hold<VE, 8 / VE, 64>, ABF, RBF>(a, grad, st);
-  if (a.d <= 1024) return launch<Hold<VE, 16 / VE, 64>, ABF, RBF>(a, grad, st);
-  if (a.d <= 2048) return launch<Hold<VE, 8 / VE, 256>, ABF, RBF>(a, grad, st);
-  if (a.d <= 4096) return launch<Hold<VE, 8 / VE, 512>, ABF, RBF>(a, grad, st);
-  if (a.d <= 8192) return launch<Hold<VE, 8 / VE, 1024>, ABF, RBF>(a, grad, st);
-  return launch<Hold<VE, 16 / VE, 1024>, ABF, RBF>(a, grad, st);
+  if (a.d <= 128) return launch<ABF, RBF, Hold<VE, 8 / VE, 16>>(a, grad, st);
+  if (a.d <= 256) return launch<ABF, RBF, Hold<VE, 8 / VE, 32>>(a, grad, st);
+  if (a.d <= 512) return launch<ABF, RBF, Hold<VE, 8 / VE, 64>>(a, grad, st);
+  if (a.d <= 1024) return launch<ABF, RBF, Hold<VE, 16 / VE, 64>>(a, grad, st);
+  if (a.d <= 2048) return launch<ABF, RBF, Hold<VE, 8 / VE, 256>>(a, grad, st);
+  if (a.d <= 4096) return launch<ABF, RBF, Hold<VE, 8 / VE, 512>>(a, grad, st);
+  if (a.d <= 8192)
+    return launch<ABF, RBF, Hold<VE, 16 / VE, 512>, Hold<VE, 8 / VE, 1024>>(a, grad, st);
+  return launch<ABF, RBF, Hold<VE, 16 / VE, 1024>>(a, grad, st);
 }
 
 // 16-byte accesses need every row of every tensor to start on 16 bytes.
