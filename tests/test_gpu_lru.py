@@ -115,7 +115,23 @@ def backward(t, states, **kw):
                            mask=t["mask"], reset=t["reset"], c=C, **kw)
 
 
-def check(t):
+def largest_gradient(t):
+    """The largest gradient of a state in [B, d], what a rounding on the way to dh0
+    is relative to."""
+    la = -C * torch.nn.functional.softplus(t["lam"].double()) * torch.sigmoid(t["r"].double())
+    a, G, most = torch.exp(la), t["dh_last"].double(), t["dh_last"].double().abs()
+    for k in reversed(range(a.shape[0])):
+        new = t["dH"][k].double() + G
+        most = torch.maximum(most, new.abs())
+        G = a[k] * new
+        if t["reset"] is not None:
+            G = torch.where((t["reset"][k] != 0)[:, None], 0.0, G)
+        if t["mask"] is not None:
+            G = torch.where((t["mask"][k] != 0)[:, None], new - t["dH"][k].double(), G)
+    return most.clamp(min=1.0)
+
+
+def check(t, dh0_scale=None):
     H, h_last, ref, lam_mag = plain(t)
     d = dev(t)
     fw = forward(d)
@@ -123,8 +139,9 @@ def check(t):
     torch.cuda.synchronize()
     close("H", fw["H"], H)
     close("h_last", fw["h_last"], h_last)
-    for n in ("x", "r", "i", "h0"):
+    for n in ("x", "r", "i"):
         close("d" + n, g["d" + n], ref[n])
+    close("dh0", g["dh0"], ref["h0"], dh0_scale)
     close("dlam", g["dlam"], ref["lam"], lam_mag + 1e-30)
     return fw, g
 
@@ -145,6 +162,18 @@ def test_values_and_gradients(L, B, d, dtype):
 @pytest.mark.parametrize("L,B,d", [(1, 3, 5), (20, 3, 64), (131, 4, 34), (700, 3, 65)])
 def test_padding_and_documents(L, B, d, mask, reset, dtype):
     check(inputs(L, B, d, dtype, 3 * L + B, mask, reset))
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("marks", [False, True])
+@pytest.mark.parametrize("L,B,d", [(70, 514, 66), (72, 1030, 6), (90, 1030, 3), (200, 600, 4),
+                                   (600, 260, 2), (4000, 1, 8), (3001, 2, 66)])
+def test_many_and_few_channels(L, B, d, marks, dtype):
+    """Every way to cut a call: small and large workgroups, one and two channels
+    a lane, one and several segments, chunks.  Among this many channels some
+    have a dh0 far below the gradients it is made of."""
+    t = inputs(L, B, d, dtype, L + B, marks, marks)
+    check(t, largest_gradient(t))
 
 
 @pytest.mark.parametrize("dtype", [F32, B16])
