@@ -100,6 +100,35 @@ __device__ __forceinline__ Span row_span(const typename Elem<BF16>::T* z, int V)
   return s;
 }
 
+// ------------------------------------------------------------ between lanes
+// x of lane l ^ O, where it can be had without LDS for O up to 15; every lane of
+// the wave takes part.
+template <int O>
+__device__ __forceinline__ unsigned lane_xor(unsigned x) {
+  constexpr int dpp = O == 1 ? 0xB1 : O == 2 ? 0x4E : O == 3 ? 0x1B  // within four lanes
+                      : O == 7 ? 0x141 : O == 15 ? 0x140              // mirrored in 8, 16
+                      : O == 8 ? 0x128 : 0;                           // rotated by 8 in 16
+  if constexpr (O == 4)
+    return lane_xor<3>(lane_xor<7>(x));
+  else if constexpr (dpp != 0)
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, dpp, 0xf, 0xf, true);
+  else
+    return (unsigned)__shfl_xor((int)x, O);
+}
+// Of LANES consecutive lanes, the same in each: pairs, fours, then mirrored eights
+// and sixteens.
+template <int LANES, typename F>
+__device__ __forceinline__ float lanes_reduce(float x, F f) {
+  const auto with = [&](unsigned o) { x = f(x, __uint_as_float(o)); };
+  if constexpr (LANES > 1) with(lane_xor<1>(__float_as_uint(x)));
+  if constexpr (LANES > 2) with(lane_xor<2>(__float_as_uint(x)));
+  if constexpr (LANES > 4) with(lane_xor<7>(__float_as_uint(x)));
+  if constexpr (LANES > 8) with(lane_xor<15>(__float_as_uint(x)));
+  if constexpr (LANES > 16) with(lane_xor<16>(__float_as_uint(x)));
+  if constexpr (LANES > 32) with(lane_xor<32>(__float_as_uint(x)));
+  return x;
+}
+
 // ------------------------------------------------------- running statistics
 // Maximum m, s = sum 2^x and t = sum 2^x x with x = (z - m) k, k = log2(e) / T.
 // base is m, or 0 while there is nothing above -inf (z - base is then -inf and
@@ -129,15 +158,6 @@ struct Run {
       if constexpr (ENT) t = fmaf(e, fmaxf(x, kLowExp), t);
     }
   }
-  __device__ __forceinline__ void join(const Run& o, float k) {
-    Run a = *this, b = o;
-    const float nm = fmaxf(a.m, b.m);
-    a.to(nm, k);
-    b.to(nm, k);
-    *this = a;
-    s += b.s;
-    if constexpr (ENT) t += b.t;
-  }
 };
 
 template <bool ENT>
@@ -158,22 +178,26 @@ __device__ __forceinline__ Run<ENT> run_load(const float* p) {
 
 // The statistics of a workgroup's threads, the same in every thread; always in
 // the same order.  lds: 3 floats a wave; barriers inside.
+template <int LANES, bool ENT>
+__device__ __forceinline__ void run_lanes(Run<ENT>& r, float k) {
+  r.to(lanes_reduce<LANES>(r.m, [](float a, float b) { return fmaxf(a, b); }), k);
+  // not contracted with the factors in front: a lane's own product would enter
+  // unrounded, its neighbour's rounded, and the lanes' sums would differ
+  const auto add = [](float a, float b) {
+#pragma clang fp contract(off)
+    return a + b;
+  };
+  r.s = lanes_reduce<LANES>(r.s, add);
+  if constexpr (ENT) r.t = lanes_reduce<LANES>(r.t, add);
+}
 template <int THREADS, bool ENT>
 __device__ __forceinline__ Run<ENT> run_block(Run<ENT> r, float k, float* lds) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    Run<ENT> b;
-    b.m = __shfl_xor(r.m, o);
-    b.s = __shfl_xor(r.s, o);
-    if constexpr (ENT) b.t = __shfl_xor(r.t, o);
-    r.join(b, k);
-  }
+  run_lanes<64>(r, k);
   constexpr int W = THREADS / 64;
   if ((threadIdx.x & 63) == 0) run_store(lds + 3 * (threadIdx.x >> 6), r);
   __syncthreads();
-  r = run_load<ENT>(lds);
-#pragma unroll
-  for (int w = 1; w < W; ++w) r.join(run_load<ENT>(lds + 3 * w), k);
+  r = run_load<ENT>(lds + 3 * (threadIdx.x & (W - 1)));
+  run_lanes<W>(r, k);
   __syncthreads();
   return r;
 }
@@ -192,19 +216,23 @@ __device__ __forceinline__ bool top_better(unsigned k, unsigned i, unsigned k2, 
   return k > k2 || (k == k2 && i < i2);
 }
 
-// A wave's 64 keys, the largest in lane 0.
-__device__ __forceinline__ unsigned wave_sort(unsigned key) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int size = 2; size <= 64; size <<= 1) {
-#pragma unroll
-    for (int step = size >> 1; step > 0; step >>= 1) {
-      const unsigned o = __shfl_xor(key, step);
-      const bool larger = ((lane & size) == 0) == ((lane & step) == 0);
-      key = larger ? max(key, o) : min(key, o);
-    }
-  }
+// A wave's 64 keys, the largest in lane 0: runs of SIZE lanes are sorted from two
+// of half the size, first against each other's mirror image.
+template <int O>
+__device__ __forceinline__ unsigned sort_step(unsigned key) {
+  constexpr int high = O > 31 ? 32 : O > 15 ? 16 : O > 7 ? 8 : O > 3 ? 4 : O > 1 ? 2 : 1;
+  const unsigned o = lane_xor<O>(key);
+  return threadIdx.x & high ? min(key, o) : max(key, o);
+}
+template <int STEP>
+__device__ __forceinline__ unsigned sort_steps(unsigned key) {
+  if constexpr (STEP > 0) return sort_steps<STEP / 2>(sort_step<STEP>(key));
   return key;
+}
+template <int SIZE = 64>
+__device__ __forceinline__ unsigned wave_sort(unsigned key) {
+  if constexpr (SIZE > 2) key = wave_sort<SIZE / 2>(key);
+  return sort_steps<SIZE / 4>(sort_step<SIZE - 1>(key));
 }
 
 // Candidates for a row's best K, found by one of a workgroup's W waves: in its
@@ -430,22 +458,29 @@ __device__ __forceinline__ float row_logprob(const RowStats& r, float z, float i
 }
 
 // ------------------------------------------------- token log probabilities
+// The row's token and its logit: asked for before the row is read, and while its
+// sums are joined.
+template <bool BF16>
+struct Scored {
+  int64_t tok;
+  float z = 0.f;
+  bool inside = false;
+  __device__ __forceinline__ Scored(const LogprobArgs& a, int row) : tok(a.tokens[row]) {}
+  __device__ __forceinline__ void gather(const LogprobArgs& a,
+                                         const typename Elem<BF16>::T* row) {
+    inside = tok >= 0 && tok < a.r.V;
+    if (inside) z = Elem<BF16>::get(row[tok]);
+  }
+};
 template <bool BF16>
 __device__ __forceinline__ void logprob_write(const LogprobArgs& a, int row, float m, float s,
-                                              float t, float inv_t) {
-  using E = Elem<BF16>;
+                                              float t, float inv_t, const Scored<BF16>& token) {
   const RowStats st = row_stats(m, s);
   a.stats[2LL * row] = m;
   a.stats[2LL * row + 1] = s;
   // H = log S - sum e^x x / S (t is in units of log 2); 0 where nothing is possible
   a.entropy[row] = s == 0.f ? 0.f : st.log_s - kLn2 * t / s;
-  const int64_t tok = a.tokens[row];
-  float lp = 0.f;
-  if (tok >= 0 && tok < a.r.V) {
-    const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
-    lp = row_logprob(st, E::get(z[tok]), inv_t);
-  }
-  a.logprob[row] = lp;
+  a.logprob[row] = token.inside ? row_logprob(st, token.z, inv_t) : 0.f;
 }
 
 __device__ __forceinline__ void top_write(const LogprobArgs& a, int row, const RowStats& st,
@@ -459,13 +494,16 @@ __device__ __forceinline__ void top_write(const LogprobArgs& a, int row, const R
 // statistics and its best alternatives go to the workspace, [row, part] of 4
 // floats, then [row, part, K] pairs.
 //
-// Without alternatives it reads at 4.8 TB/s (2048 x 65536 bf16, 56 us) and is
-// bound by that.  With five, 1000 x 30011 fp32 takes 40 us (3.0 TB/s): the first
+// Without alternatives it reads at 4.9 TB/s (2048 x 65536 bf16, 54 us) and is
+// bound by that.  With five, 1000 x 30011 fp32 takes 35 us (3.5 TB/s): the first
 // vectors of a row fill the lists before there is a bound, and all rows are at it
-// at the same time.  Twenty of 4 x 131072 bf16, in 64 parts a row, take 12.6 us and
-// 7.2 to join: launches and waits, one after the other.
+// at the same time.  Twenty of 4 x 131072 bf16, in eight parts a row, take 11.5 us and
+// 6.4 to join: launches and waits, one after the other.  Loads a round ahead were
+// slower in every case (1000 x 30011 26 -> 27 us, with alternatives 39 -> 52).
+// Six waves on a SIMD rather than the five that the compiler would leave: three
+// workgroups fit a CU (4096 x 32768 bf16, five alternatives, 90 -> 80 us).
 template <bool BF16, int THREADS, int U, bool TOP>
-__global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a, int parts) {
+__global__ __launch_bounds__(THREADS, TOP && BF16 ? 6 : 1) void logprob_kernel(LogprobArgs a, int parts) {
   using E = Elem<BF16>;
   constexpr int W = THREADS / 64, kPitch = 64 * E::VE + kFoundRest;
   __shared__ float red[3 * W];
@@ -479,18 +517,20 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a, int par
   for (long long it = blockIdx.x; it < items; it += gridDim.x) {
     const int row = (int)(it / parts), part = (int)(it - (long long)row * parts);
     const auto* z = static_cast<const typename E::T*>(a.r.z) + (long long)row * a.r.ld;
+    Scored<BF16> token(a, row);
     Found<W> top{lists + (TOP ? wave * kPitch : 0), &floor, bounds, a.top};
     if constexpr (TOP) {
       if (threadIdx.x == 0) floor = 0;
       __syncthreads();
     }
     Run<true> run = part_stats<BF16, THREADS, U, true, TOP>(z, a.r.V, part, parts, k, top);
+    if (parts == 1) token.gather(a, z);
     if constexpr (TOP) {
       if ((threadIdx.x & 63) == 0) count[wave] = top.n;
     }
     run = run_block<THREADS>(run, k, red);  // its barriers make the lists visible
     if (parts == 1) {
-      if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
+      if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t, token);
       if constexpr (TOP) {
         const RowStats st = row_stats(run.m, run.s);
         top_merge<THREADS>(lists, kPitch, W, count, floor, a.top, kept, kRoom, &kept_n,
@@ -534,17 +574,12 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a, int pa
         lists[e] = wl[(long long)row * parts * a.top + e];
     }
     // one part a lane, joined across the wave; every wave does the same
+    Scored<BF16> token(a, row);
     Run<true> run;
     if (lane < parts) run = run_load<true>(ws + 4 * ((long long)row * parts + lane));
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      Run<true> b;
-      b.m = __shfl_xor(run.m, o);
-      b.s = __shfl_xor(run.s, o);
-      b.t = __shfl_xor(run.t, o);
-      run.join(b, k);
-    }
-    if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t);
+    token.gather(a, static_cast<const typename Elem<BF16>::T*>(a.r.z) + (long long)row * a.r.ld);
+    run_lanes<64>(run, k);
+    if (threadIdx.x == 0) logprob_write<BF16>(a, row, run.m, run.s, run.t, inv_t, token);
     if constexpr (TOP) {
       // K / parts entries of every list are at least as good as the least of the
       // lists' K / parts-th
@@ -782,8 +817,7 @@ struct Teacher {
       // a NaN that fmaxf drops comes back in the sum
       if (e < a.K && col[p] >= 0) m = fmaxf(m, t[p]);
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    m = lanes_reduce<64>(m, [](float a, float b) { return fmaxf(a, b); });
     if (lane == 0) scratch[wave] = m;
     __syncthreads();
     for (int w = 0; w < W; ++w) m = fmaxf(m, scratch[w]);
@@ -798,8 +832,7 @@ struct Teacher {
       s += t[p];
       any |= col[p] >= 0;
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
+    s = lanes_reduce<64>(s, [](float a, float b) { return a + b; });
     if (lane == 0) scratch[wave] = s;
     const int some = __syncthreads_or(any);
     s = 0.f;
@@ -830,8 +863,7 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, const float*
     // p = 0 (too small for fp32, or no entry) adds 0; a NaN stays one
     if (p != 0.f) loss += p * (logf(p) - row_logprob(st, zs[e], inv_t));
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) loss += __shfl_xor(loss, o);
+  loss = lanes_reduce<64>(loss, [](float a, float b) { return a + b; });
   if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = loss;
   __syncthreads();
   loss = 0.f;
@@ -844,11 +876,11 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, const float*
 // is written.  parts > 1 with STATS: only the part's statistics are, into the
 // workspace.
 //
-// Bound by memory.  4096 x 65536 bf16: the loss 108 us (5.0 TB/s), its gradient 230
-// (4.7 TB/s read and written), both at once 280: a row's second read comes from
+// Bound by memory.  4096 x 65536 bf16: the loss 97 us (5.5 TB/s), its gradient 228
+// (4.7 TB/s read and written), both at once 270: a row's second read comes from
 // the caches, which the rows that run at a time (three to a CU) fit.  Holding a row in
 // registers between its two uses was slower: only one then fits a CU, and its
-// loads stop while it writes.  515 x 30011 fp32: 18.6 and 25 us; all rows run at
+// loads stop while it writes.  515 x 30011 fp32: 16 and 25 us; all rows run at
 // the same time there, and none reads while they join their sums and the teacher's.
 template <bool BF16, int THREADS, int U, bool STATS, bool GRAD>
 __global__ __launch_bounds__(THREADS, 6) void distill_kernel(DistillArgs a, int parts) {
@@ -929,13 +961,7 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a, int pa
     Run<false> run;
     if (lane < parts) run = run_load<false>(ws + 4 * ((long long)row * parts + lane));
     teacher.gather(a, z);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      Run<false> b;
-      b.m = __shfl_xor(run.m, o);
-      b.s = __shfl_xor(run.s, o);
-      run.join(b, k);
-    }
+    run_lanes<64>(run, k);
     const RowStats st = row_stats(run.m, run.s);
     teacher.probabilities(a, cols, probs, zs, red, k);
     const float loss = distill_loss<256>(a, probs, zs, red, st, inv_t);
