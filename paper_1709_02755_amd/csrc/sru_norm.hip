@@ -10,6 +10,7 @@
 // bf16 beside an fp32 residual: 50 us for 235 MB (4.7 TB/s) and 91 us for 369 MB (4.0
 // TB/s, 29 % of what the vector units can do); 8 x 1024 bf16: 4.6 us, a launch.
 #include "sru_device.h"
+#include "sru_lanes.h"
 #include "sru_lm.h"
 
 namespace sru {
@@ -173,8 +174,7 @@ __device__ __forceinline__ void store_row(const void* p, long long off, int d,
 // The sum over a row's threads, in each of them, always in the same order.
 template <class H>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
-#pragma unroll
-  for (int o = 1; o < (H::LANES < 64 ? H::LANES : 64); o <<= 1) v += __shfl_xor(v, o);
+  v = lanes_sum<(H::LANES < 64 ? H::LANES : 64)>(v);
   if constexpr (H::NW > 1) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();

@@ -8,6 +8,7 @@
 // are bound by reading (and writing) the rows.
 #include <math.h>
 
+#include "sru_lanes.h"
 #include "sru_lm.h"
 
 namespace sru {
@@ -100,35 +101,6 @@ __device__ __forceinline__ Span row_span(const typename Elem<BF16>::T* z, int V)
   return s;
 }
 
-// ------------------------------------------------------------ between lanes
-// x of lane l ^ O, where it can be had without LDS for O up to 15; every lane of
-// the wave takes part.
-template <int O>
-__device__ __forceinline__ unsigned lane_xor(unsigned x) {
-  constexpr int dpp = O == 1 ? 0xB1 : O == 2 ? 0x4E : O == 3 ? 0x1B  // within four lanes
-                      : O == 7 ? 0x141 : O == 15 ? 0x140              // mirrored in 8, 16
-                      : O == 8 ? 0x128 : 0;                           // rotated by 8 in 16
-  if constexpr (O == 4)
-    return lane_xor<3>(lane_xor<7>(x));
-  else if constexpr (dpp != 0)
-    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, dpp, 0xf, 0xf, true);
-  else
-    return (unsigned)__shfl_xor((int)x, O);
-}
-// Of LANES consecutive lanes, the same in each: pairs, fours, then mirrored eights
-// and sixteens.
-template <int LANES, typename F>
-__device__ __forceinline__ float lanes_reduce(float x, F f) {
-  const auto with = [&](unsigned o) { x = f(x, __uint_as_float(o)); };
-  if constexpr (LANES > 1) with(lane_xor<1>(__float_as_uint(x)));
-  if constexpr (LANES > 2) with(lane_xor<2>(__float_as_uint(x)));
-  if constexpr (LANES > 4) with(lane_xor<7>(__float_as_uint(x)));
-  if constexpr (LANES > 8) with(lane_xor<15>(__float_as_uint(x)));
-  if constexpr (LANES > 16) with(lane_xor<16>(__float_as_uint(x)));
-  if constexpr (LANES > 32) with(lane_xor<32>(__float_as_uint(x)));
-  return x;
-}
-
 // ------------------------------------------------------- running statistics
 // Maximum m, s = sum 2^x and t = sum 2^x x with x = (z - m) k, k = log2(e) / T.
 // base is m, or 0 while there is nothing above -inf (z - base is then -inf and
@@ -180,15 +152,9 @@ __device__ __forceinline__ Run<ENT> run_load(const float* p) {
 // the same order.  lds: 3 floats a wave; barriers inside.
 template <int LANES, bool ENT>
 __device__ __forceinline__ void run_lanes(Run<ENT>& r, float k) {
-  r.to(lanes_reduce<LANES>(r.m, [](float a, float b) { return fmaxf(a, b); }), k);
-  // not contracted with the factors in front: a lane's own product would enter
-  // unrounded, its neighbour's rounded, and the lanes' sums would differ
-  const auto add = [](float a, float b) {
-#pragma clang fp contract(off)
-    return a + b;
-  };
-  r.s = lanes_reduce<LANES>(r.s, add);
-  if constexpr (ENT) r.t = lanes_reduce<LANES>(r.t, add);
+  r.to(lanes_max<LANES>(r.m), k);
+  r.s = lanes_sum<LANES>(r.s);
+  if constexpr (ENT) r.t = lanes_sum<LANES>(r.t);
 }
 template <int THREADS, bool ENT>
 __device__ __forceinline__ Run<ENT> run_block(Run<ENT> r, float k, float* lds) {
@@ -817,7 +783,7 @@ struct Teacher {
       // a NaN that fmaxf drops comes back in the sum
       if (e < a.K && col[p] >= 0) m = fmaxf(m, t[p]);
     }
-    m = lanes_reduce<64>(m, [](float a, float b) { return fmaxf(a, b); });
+    m = lanes_max<64>(m);
     if (lane == 0) scratch[wave] = m;
     __syncthreads();
     for (int w = 0; w < W; ++w) m = fmaxf(m, scratch[w]);
@@ -832,7 +798,7 @@ struct Teacher {
       s += t[p];
       any |= col[p] >= 0;
     }
-    s = lanes_reduce<64>(s, [](float a, float b) { return a + b; });
+    s = lanes_sum<64>(s);
     if (lane == 0) scratch[wave] = s;
     const int some = __syncthreads_or(any);
     s = 0.f;
@@ -863,7 +829,7 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, const float*
     // p = 0 (too small for fp32, or no entry) adds 0; a NaN stays one
     if (p != 0.f) loss += p * (logf(p) - row_logprob(st, zs[e], inv_t));
   }
-  loss = lanes_reduce<64>(loss, [](float a, float b) { return a + b; });
+  loss = lanes_sum<64>(loss);
   if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = loss;
   __syncthreads();
   loss = 0.f;
