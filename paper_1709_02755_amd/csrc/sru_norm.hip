@@ -7,8 +7,10 @@
 // in 16-byte loads where the rows allow, its sums are taken there, and the
 // results leave rounded once.  The gradient works x' out again from x, y and z
 // rather than reading x_out, so that no rounded value enters it.  16384 x 1024,
-// bf16 beside an fp32 residual: 50 us for 235 MB (4.7 TB/s) and 91 us for 369 MB (4.0
+// bf16 beside an fp32 residual: 50 us for 235 MB (4.7 TB/s) and 88 us for 369 MB (4.2
 // TB/s, 29 % of what the vector units can do); 8 x 1024 bf16: 4.6 us, a launch.
+#include <type_traits>
+
 #include "sru_device.h"
 #include "sru_lanes.h"
 #include "sru_lm.h"
@@ -16,21 +18,49 @@
 namespace sru {
 namespace {
 
+// 16 bytes in memory, and where an element may lie rather than on 16 bytes.
 typedef unsigned Quad __attribute__((ext_vector_type(4)));
 template <bool BF16>
 struct Mem {
   using T = float;
+  typedef Quad Loose __attribute__((aligned(4)));
 };
 template <>
 struct Mem<true> {
   using T = uint16_t;
+  typedef Quad Loose __attribute__((aligned(2)));
 };
 
 // VE consecutive elements to and from floats; 16-byte accesses (two for 8
-// fp32 values) unless VE is 1.
-template <bool BF16, int VE>
-__device__ __forceinline__ void load(const typename Mem<BF16>::T* p, float* f) {
-  if constexpr (VE == 1) {
+// fp32 values) unless VE is 1.  TAIL: anywhere, and only the first `left` of them
+// may be there; the others are 0.
+template <bool BF16, int VE, bool TAIL>
+__device__ __forceinline__ void load(const typename Mem<BF16>::T* p, int left, float* f) {
+  constexpr int E = BF16 ? 8 : 4;  // of 16 bytes
+  if constexpr (TAIL) {
+    static_assert(VE % E == 0, "16 bytes");
+    if (left >= VE) {
+#pragma unroll
+      for (int i = 0; i < VE; i += E) {
+        const Quad q = *reinterpret_cast<const typename Mem<BF16>::Loose*>(p + i);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if constexpr (BF16) {
+            f[2 * w] = __uint_as_float(q[w] << 16);
+            f[2 * w + 1] = __uint_as_float(q[w] & 0xffff0000u);
+          } else {
+            f[i + w] = __uint_as_float(q[w]);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        f[i] = 0.f;
+        if (i < left) load<BF16, 1, false>(p + i, 1, f + i);
+      }
+    }
+  } else if constexpr (VE == 1) {
     if constexpr (BF16) f[0] = __uint_as_float((unsigned)*p << 16);
     else f[0] = *p;
   } else if constexpr (BF16) {
@@ -54,9 +84,14 @@ __device__ __forceinline__ void load(const typename Mem<BF16>::T* p, float* f) {
   }
 }
 // LAST: past the caches, for what is not read again soon.
-template <bool BF16, int VE, bool LAST = false>
-__device__ __forceinline__ void store(typename Mem<BF16>::T* p, const float* f) {
-  if constexpr (VE == 1) {
+template <bool BF16, int VE, bool TAIL, bool LAST>
+__device__ __forceinline__ void store(typename Mem<BF16>::T* p, int left, const float* f) {
+  using Q = std::conditional_t<TAIL, typename Mem<BF16>::Loose, Quad>;
+  if (TAIL && left < VE) {
+#pragma unroll
+    for (int i = 0; i < VE; ++i)
+      if (i < left) store<BF16, 1, false, false>(p + i, 1, f + i);
+  } else if constexpr (VE == 1) {
     if constexpr (BF16) *p = __builtin_bit_cast(uint16_t, (__bf16)f[0]);
     else *p = f[0];
   } else if constexpr (BF16) {
@@ -66,15 +101,15 @@ __device__ __forceinline__ void store(typename Mem<BF16>::T* p, const float* f) 
       w[i] = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)f[2 * i]) |
              ((unsigned)__builtin_bit_cast(uint16_t, (__bf16)f[2 * i + 1]) << 16);
     const Quad q = {w[0], w[1], w[2], w[3]};
-    if constexpr (LAST) __builtin_nontemporal_store(q, reinterpret_cast<Quad*>(p));
-    else *reinterpret_cast<Quad*>(p) = q;
+    if constexpr (LAST) __builtin_nontemporal_store(q, reinterpret_cast<Q*>(p));
+    else *reinterpret_cast<Q*>(p) = q;
   } else {
 #pragma unroll
     for (int i = 0; i < VE; i += 4) {
       const Quad q = {__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]),
                       __float_as_uint(f[i + 3])};
-      if constexpr (LAST) __builtin_nontemporal_store(q, reinterpret_cast<Quad*>(p + i));
-      else *reinterpret_cast<Quad*>(p + i) = q;
+      if constexpr (LAST) __builtin_nontemporal_store(q, reinterpret_cast<Q*>(p + i));
+      else *reinterpret_cast<Q*>(p + i) = q;
     }
   }
 }
@@ -83,9 +118,11 @@ __device__ __forceinline__ void store(typename Mem<BF16>::T* p, const float* f) 
 // columns, the chunks of a row dealt to its threads in turn.  Rows of up to a
 // wave (16, 32 or 64 lanes) come 256 / LANES to a workgroup; their sums need no
 // barrier.
-template <int VE_, int C_, int LANES_>
+// TAIL: a row may start between 16-byte boundaries and end inside a chunk.
+template <int VE_, int C_, int LANES_, bool TAIL_ = false>
 struct Hold {
   static constexpr int VE = VE_, C = C_, LANES = LANES_, F = VE_ * C_;
+  static constexpr bool TAIL = TAIL_;
   static constexpr int NW = LANES_ <= 64 ? 1 : LANES_ / 64;  // waves of a row
   static constexpr int ROWS = NW == 1 ? 256 / LANES_ : 1;
   static constexpr int THREADS = LANES_ * ROWS;
@@ -97,6 +134,7 @@ struct Hold {
 // F columns of a row as they lie in memory; columns past d are 0.
 template <class H, bool BF16>
 struct Raw {
+  static_assert(!H::TAIL, "rows of whole pieces, or one by one");
   static constexpr int Q = H::VE * (BF16 ? 2 : 4) / 16;  // 16-byte pieces of a chunk
   uint4 q[Q ? H::C * Q : 1];
   typename Mem<BF16>::T e[Q ? 1 : H::C];
@@ -153,7 +191,7 @@ __device__ __forceinline__ void load_row(const void* p, long long off, int d, fl
   for (int c = 0; c < H::C; ++c) {
     const int col = H::col(c);
     if (col < d) {
-      load<BF16, H::VE>(q + col, f + c * H::VE);
+      load<BF16, H::VE, H::TAIL>(q + col, d - col, f + c * H::VE);
     } else {
 #pragma unroll
       for (int j = 0; j < H::VE; ++j) f[c * H::VE + j] = 0.f;
@@ -167,7 +205,7 @@ __device__ __forceinline__ void store_row(const void* p, long long off, int d,
 #pragma unroll
   for (int c = 0; c < H::C; ++c) {
     const int col = H::col(c);
-    if (col < d) store<BF16, H::VE, LAST>(q + col, f + c * H::VE);
+    if (col < d) store<BF16, H::VE, H::TAIL, LAST>(q + col, d - col, f + c * H::VE);
   }
 }
 
@@ -282,7 +320,8 @@ norm_grad_kernel(NormArgs a) {
   for (int j = 0; j < H::F; ++j) gw_post[j] = gscale[j] = gw_pre[j] = 0.f;
 
   const long long step = (long long)gridDim.x * H::ROWS;
-  GradRow<H, ABF, RBF> row, next;
+  struct None {};
+  std::conditional_t<WHOLE, GradRow<H, ABF, RBF>, None> row, next;
   if constexpr (AHEAD) next.load(a, (long long)blockIdx.x * H::ROWS + H::sub());
   for (long long m0 = (long long)blockIdx.x * H::ROWS; m0 < a.M; m0 += step) {
     const long long m = m0 + H::sub();
@@ -480,21 +519,32 @@ hipError_t launch(const NormArgs& a, bool grad, hipStream_t st) {
 // row and needs no barrier, and past 8192; past 4096 in the forward, which has
 // registers to spare and waits for fewer waves then: 2000 x 6000 fp32 60 -> 50 us,
 // while the gradient takes 97 with 8 and 103 with 16).
-template <int VE, bool ABF, bool RBF>
+// Rows that are not whole pieces of 16 bytes take them all the same (TAIL: 16384 x
+// 1001 bf16 beside fp32, forward 93 -> 53 us; 2000 x 6001 fp32, gradient 146 -> 96),
+// but for the gradient up to 2048 columns, which takes elements one by one (10154 x
+// 1277 bf16 92 us and 166 so, 5123 x 301 fp32 22 and 24: pieces that lie on odd
+// elements are slow to store).
+template <int VE, bool ABF, bool RBF, bool TAIL>
 hipError_t by_width(const NormArgs& a, bool grad, hipStream_t st) {
-  if (a.d <= 128) return launch<ABF, RBF, Hold<VE, 8 / VE, 16>>(a, grad, st);
-  if (a.d <= 256) return launch<ABF, RBF, Hold<VE, 8 / VE, 32>>(a, grad, st);
-  if (a.d <= 512) return launch<ABF, RBF, Hold<VE, 8 / VE, 64>>(a, grad, st);
-  if (a.d <= 1024) return launch<ABF, RBF, Hold<VE, 16 / VE, 64>>(a, grad, st);
-  if (a.d <= 2048) return launch<ABF, RBF, Hold<VE, 8 / VE, 256>>(a, grad, st);
-  if (a.d <= 4096) return launch<ABF, RBF, Hold<VE, 8 / VE, 512>>(a, grad, st);
+  constexpr int C = 8 / VE, G = TAIL ? 1 : VE, D = 8 / G;
+  if (a.d <= 128)
+    return launch<ABF, RBF, Hold<VE, C, 16, TAIL>, Hold<G, D, 16>>(a, grad, st);
+  if (a.d <= 256)
+    return launch<ABF, RBF, Hold<VE, C, 32, TAIL>, Hold<G, D, 32>>(a, grad, st);
+  if (a.d <= 512)
+    return launch<ABF, RBF, Hold<VE, C, 64, TAIL>, Hold<G, D, 64>>(a, grad, st);
+  if (a.d <= 1024)
+    return launch<ABF, RBF, Hold<VE, 2 * C, 64, TAIL>, Hold<G, 2 * D, 64>>(a, grad, st);
+  if (a.d <= 2048)
+    return launch<ABF, RBF, Hold<VE, C, 256, TAIL>, Hold<G, D, 256>>(a, grad, st);
+  if (a.d <= 4096) return launch<ABF, RBF, Hold<VE, C, 512, TAIL>>(a, grad, st);
   if (a.d <= 8192)
-    return launch<ABF, RBF, Hold<VE, 16 / VE, 512>, Hold<VE, 8 / VE, 1024>>(a, grad, st);
-  return launch<ABF, RBF, Hold<VE, 16 / VE, 1024>>(a, grad, st);
+    return launch<ABF, RBF, Hold<VE, 2 * C, 512, TAIL>, Hold<VE, C, 1024, TAIL>>(a, grad, st);
+  return launch<ABF, RBF, Hold<VE, 2 * C, 1024, TAIL>>(a, grad, st);
 }
 
-// 16-byte accesses need every row of every tensor to start on 16 bytes.
-bool vector_ok(const NormArgs& a) {
+// Whether every row of every tensor is whole pieces of 16 bytes.
+bool whole_pieces(const NormArgs& a) {
   const int ve = a.act_bf16 ? 8 : 4;
   if (a.d % ve) return false;
   auto rows = [](const Rows& r, bool bf16) {
@@ -507,13 +557,16 @@ bool vector_ok(const NormArgs& a) {
          vec(a.w_post) && vec(a.scale) && vec(a.w_pre);
 }
 
+template <int VE, bool ABF, bool RBF>
+hipError_t by_pieces(const NormArgs& a, bool grad, hipStream_t st) {
+  return whole_pieces(a) ? by_width<VE, ABF, RBF, false>(a, grad, st)
+                         : by_width<VE, ABF, RBF, true>(a, grad, st);
+}
+
 hipError_t dispatch(const NormArgs& a, bool grad, hipStream_t st) {
-  const bool v = vector_ok(a);
-  if (!a.act_bf16)
-    return v ? by_width<4, false, false>(a, grad, st) : by_width<1, false, false>(a, grad, st);
-  if (!a.res_bf16)
-    return v ? by_width<8, true, false>(a, grad, st) : by_width<1, true, false>(a, grad, st);
-  return v ? by_width<8, true, true>(a, grad, st) : by_width<1, true, true>(a, grad, st);
+  if (!a.act_bf16) return by_pieces<4, false, false>(a, grad, st);
+  if (!a.res_bf16) return by_pieces<8, true, false>(a, grad, st);
+  return by_pieces<8, true, true>(a, grad, st);
 }
 
 }  // namespace

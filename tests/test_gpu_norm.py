@@ -229,6 +229,40 @@ def test_strided_rows_and_own_memory(d, pitch, offset, act, res):
     assert torch.equal(f3["o"], f2["o"])
 
 
+@pytest.mark.parametrize("act,res", TYPES)
+@pytest.mark.parametrize("d,pitch,offset", [(33, 39, 3), (1001, 1003, 1), (4099, 4100, 2),
+                                            (8191, 8193, 7)])
+def test_nothing_beside_ragged_rows(d, pitch, offset, act, res):
+    """Outputs whose rows end inside 16 bytes and start between them: what lies
+    between the rows, before and after them stays."""
+    M = 6
+    t = inputs(M, d, act, res, 8)
+    mag = magnitudes(t, lm.GATE_SILU)
+    t = dev(t)
+    p = dict(w_post=t["w_post"], scale=t["scale"], w_pre=t["w_pre"], eps=EPS)
+    fw, g = run(t, lm.GATE_SILU)
+    bufs = {}
+
+    def out_of(n, dtype):
+        buf = torch.full((M * pitch + offset + 8,), 7.0, dtype=dtype, device="cuda")
+        bufs[n] = buf
+        return buf[offset:offset + M * pitch].view(M, pitch)[:, :d]
+
+    f2 = lm.residual_norm_forward(t["x"], t["y"], z=t["z"], **p,
+                                  out=dict(x_out=out_of("x_out", res), o=out_of("o", act)))
+    g2 = lm.residual_norm_backward(t["x"], t["y"], f2["rstd"], t["dx_out"], t["do"], z=t["z"], **p,
+                                   out=dict(dx=out_of("dx", res), dy=out_of("dy", act),
+                                            dz=out_of("dz", act)))
+    for n in ("x_out", "o"):
+        close(n, f2[n], fw[n].cpu().double(), mag[n])
+    for n in ("x", "y", "z", "w_post", "scale", "w_pre"):
+        close(n, g2["d" + n], g["d" + n].cpu().double(), mag[n])
+    for n, buf in bufs.items():
+        rest = buf[offset:offset + M * pitch].view(M, pitch)[:, d:]
+        assert bool((rest == 7.0).all()), n
+        assert bool((buf[:offset] == 7.0).all()) and bool((buf[-8:] == 7.0).all()), n
+
+
 def test_leading_dimensions():
     t = dev(inputs(12, 40, B16, B16, 9))
     fw, g = run(t, lm.GATE_SILU)
