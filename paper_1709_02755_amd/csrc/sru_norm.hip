@@ -4,11 +4,11 @@
 // with rstd(v) = 1 / sqrt(mean(v^2) + eps), and its gradient.
 //
 // Both are bound by memory: a row's tensors are read once into registers, all
-// in 16-byte loads where the rows allow, its sums are taken there, and the
+// in 16-byte loads (but see by_width), its sums are taken there, and the
 // results leave rounded once.  The gradient works x' out again from x, y and z
 // rather than reading x_out, so that no rounded value enters it.  16384 x 1024,
 // bf16 beside an fp32 residual: 50 us for 235 MB (4.7 TB/s) and 88 us for 369 MB (4.2
-// TB/s, 29 % of what the vector units can do); 8 x 1024 bf16: 4.6 us, a launch.
+// TB/s); 8 x 1024 bf16: 4.4 us, a launch.
 #include <type_traits>
 
 #include "sru_device.h"
