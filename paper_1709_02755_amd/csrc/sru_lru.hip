@@ -920,7 +920,9 @@ size_t lru_grad_workspace_bytes(int L, int B, int d) {
 }
 
 long long lru_blocks(int L, int B, int d) {
-  return (long long)B * ((d + 63) / 64) * plan(L, B, d, true).nseg;  // one channel a lane
+  // one channel a lane
+  return (long long)B * ((d + 63) / 64) *
+         std::max(plan(L, B, d, false).chunks, plan(L, B, d, true).chunks);
 }
 
 hipError_t lru_launch(const LruArgs& a, hipStream_t stream) {

@@ -77,6 +77,14 @@ def test_workspace_queries():
     assert f(0, 4, 64) == 0 and b(10, 0, 64) == 0
 
 
+def test_sizes_that_fit_a_launch():
+    """What is refused by its size is what no launch takes, not a long sequence of
+    many channels."""
+    f, b = sru.lib().sru_lru_forward_workspace_bytes, sru.lib().sru_lru_backward_workspace_bytes
+    assert b(100000, 64, 2048) == 4 * 64 * 2048 and f(100000, 64, 2048) == 0
+    assert b(1, 1 << 23, 1) == 0        # 2^23 workgroups
+
+
 class Stub:
     def __init__(self):
         self.calls = []
