@@ -94,13 +94,6 @@ struct Pack<false, 1> {
   __device__ __forceinline__ float get(int) const { return u; }
   __device__ __forceinline__ void put(const float (&f)[1]) { u = f[0]; }
 };
-template <>
-struct Pack<false, 2> {
-  float2 u;
-  __device__ __forceinline__ float get(int v) const { return v ? u.y : u.x; }
-  __device__ __forceinline__ void put(const float (&f)[2]) { u = make_float2(f[0], f[1]); }
-};
-
 // Where a wave's and its lanes' channels lie: a workgroup's lanes are 64 VEC
 // features of one sequence, so that what depends on the sequence and the step
 // alone (addresses, padding, new documents) is worked out once for the wave.
@@ -830,21 +823,20 @@ Plan plan(int L, int B, int d, bool grad) {
   return p;
 }
 
-// Two channels a lane where every pair of features lies on its own size.
+// Two channels of 16 bits a lane, where every pair of features lies on its size.
 template <typename F>
 bool pairs_ok(const LruArgs& a, F each) {
   if (a.d & 1) return false;
-  const uintptr_t pair = a.bf16 ? 3 : 7;
   bool ok = true;
   each([&](const Seq& s) {
-    ok = ok && ((reinterpret_cast<uintptr_t>(s.p) & pair) == 0) && !(s.st & 1) && !(s.sb & 1);
+    ok = ok && ((reinterpret_cast<uintptr_t>(s.p) & 3) == 0) && !(s.st & 1) && !(s.sb & 1);
   });
   return ok;
 }
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 template <bool BF16, int VEC, bool FLAGS, bool WIDE>
-void launch(const LruArgs& a, const Cut& c, const Plan& p, hipStream_t st) {
+hipError_t launch(const LruArgs& a, const Cut& c, const Plan& p, hipStream_t st) {
   constexpr int W = WIDE ? kWideWaves : kWaves;
   if constexpr (!WIDE) {
     if (c.chunks > 1) {
@@ -852,15 +844,17 @@ void launch(const LruArgs& a, const Cut& c, const Plan& p, hipStream_t st) {
       hipLaunchKernelGGL((lru_maps_kernel<BF16, VEC, FLAGS, W>),
                          dim3((unsigned)c.groups * (c.chunks - 1)), dim3(64 * W), 0, st, a, c);
       timing_after(st);
+      if (hipError_t e = hipGetLastError()) return e;
     }
   }
   timing_before("lru", st);
   hipLaunchKernelGGL((lru_kernel<BF16, VEC, FLAGS, W>), dim3((unsigned)c.groups * c.chunks),
                      dim3(64 * p.waves), 0, st, a, c);
   timing_after(st);
+  return hipGetLastError();
 }
 template <bool BF16, int VEC, bool FLAGS, bool WIDE>
-void launch_grad(const LruArgs& a, const Cut& c, const Plan& p, float* sums, hipStream_t st) {
+hipError_t launch_grad(const LruArgs& a, const Cut& c, const Plan& p, float* sums, hipStream_t st) {
   constexpr int W = WIDE ? kWideGradWaves : kGradWaves;
   if constexpr (!WIDE) {
     if (c.chunks > 1) {
@@ -868,16 +862,19 @@ void launch_grad(const LruArgs& a, const Cut& c, const Plan& p, float* sums, hip
       hipLaunchKernelGGL((lru_grad_maps_kernel<BF16, VEC, FLAGS, W>),
                          dim3((unsigned)c.groups * (c.chunks - 1)), dim3(64 * W), 0, st, a, c);
       timing_after(st);
+      if (hipError_t e = hipGetLastError()) return e;
     }
   }
   timing_before("lru_grad", st);
   hipLaunchKernelGGL((lru_grad_kernel<BF16, VEC, FLAGS, W>), dim3((unsigned)c.groups * c.chunks),
                      dim3(64 * p.waves), 0, st, a, c, sums);
   timing_after(st);
+  if (hipError_t e = hipGetLastError()) return e;
   timing_before("lru_sums", st);
   hipLaunchKernelGGL(lru_sums_kernel, dim3((a.d + 63) / 64), dim3(1024), 0, st, a, sums,
                      (long long)c.chunks * a.B);
   timing_after(st);
+  return hipGetLastError();
 }
 
 // Workspace: the chunks' maps, then (gradient) the sums.
@@ -891,15 +888,11 @@ hipError_t run(const LruArgs& a, const Plan& p, bool grad, hipStream_t st) {
               a.B * ((a.d + 64 * VEC - 1) / (64 * VEC))};
   float* sums = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + maps_bytes(p, a.B, a.d));
   const bool flags = a.mask || a.reset || a.L % T;
-  if (grad && flags)
-    launch_grad<BF16, VEC, true, WIDE>(a, c, p, sums, st);
-  else if (grad)
-    launch_grad<BF16, VEC, false, WIDE>(a, c, p, sums, st);
-  else if (flags)
-    launch<BF16, VEC, true, WIDE>(a, c, p, st);
-  else
-    launch<BF16, VEC, false, WIDE>(a, c, p, st);
-  return hipGetLastError();
+  if (grad)
+    return flags ? launch_grad<BF16, VEC, true, WIDE>(a, c, p, sums, st)
+                 : launch_grad<BF16, VEC, false, WIDE>(a, c, p, sums, st);
+  return flags ? launch<BF16, VEC, true, WIDE>(a, c, p, st)
+               : launch<BF16, VEC, false, WIDE>(a, c, p, st);
 }
 
 hipError_t dispatch(const LruArgs& a, bool grad, bool pairs, hipStream_t st) {
