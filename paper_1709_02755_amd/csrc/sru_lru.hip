@@ -260,6 +260,7 @@ __device__ __forceinline__ bool decay_rates(const LruArgs& a, const Lane& n, flo
 // that one workgroup goes through, both counted in the order of the scan.
 struct Cut {
   Map* maps;  // [chunks - 1, B * d]
+  float* h0;  // [B * d], forward: what the chunks read as h0
   int nseg, each, chunks, groups;  // segments, those of a chunk, chunks, lane groups
 };
 
@@ -496,6 +497,12 @@ __global__ __launch_bounds__(64 * W, 5) void lru_maps_kernel(LruArgs a, Cut c) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Lane n = lane_of<VEC>(a, group);
   const int t0 = (chunk * W + wave) * c.each * T;
+  // h_last may be h0's own memory, and the last chunk writes it while others may
+  // not have started: they read a copy, made before any of them runs
+  if (a.h0 && chunk == 0 && wave == 0 && n.live) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) c.h0[n.chan + v] = a.h0[n.chan + v];
+  }
   float k[VEC];
   Map m[VEC];
   if (decay_rates<VEC>(a, n, sh.rates, k))
@@ -836,7 +843,7 @@ bool pairs_ok(const LruArgs& a, F each) {
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 template <bool BF16, int VEC, bool FLAGS, bool WIDE>
-hipError_t launch(const LruArgs& a, const Cut& c, const Plan& p, hipStream_t st) {
+hipError_t launch(LruArgs a, const Cut& c, const Plan& p, hipStream_t st) {
   constexpr int W = WIDE ? kWideWaves : kWaves;
   if constexpr (!WIDE) {
     if (c.chunks > 1) {
@@ -845,6 +852,7 @@ hipError_t launch(const LruArgs& a, const Cut& c, const Plan& p, hipStream_t st)
                          dim3((unsigned)c.groups * (c.chunks - 1)), dim3(64 * W), 0, st, a, c);
       timing_after(st);
       if (hipError_t e = hipGetLastError()) return e;
+      if (a.h0) a.h0 = c.h0;
     }
   }
   timing_before("lru", st);
@@ -877,20 +885,21 @@ hipError_t launch_grad(const LruArgs& a, const Cut& c, const Plan& p, float* sum
   return hipGetLastError();
 }
 
-// Workspace: the chunks' maps, then (gradient) the sums.
+// Workspace: the chunks' maps, then the state that enters (forward, where there
+// are chunks) or the sums (gradient).
 size_t maps_bytes(const Plan& p, int B, int d) {
   return align_up(sizeof(Map) * (size_t)(p.chunks - 1) * B * d);
 }
 
 template <bool BF16, int VEC, bool WIDE>
 hipError_t run(const LruArgs& a, const Plan& p, bool grad, hipStream_t st) {
-  const Cut c{static_cast<Map*>(a.workspace), p.nseg, p.each, p.chunks,
+  float* rest = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + maps_bytes(p, a.B, a.d));
+  const Cut c{static_cast<Map*>(a.workspace), rest, p.nseg, p.each, p.chunks,
               a.B * ((a.d + 64 * VEC - 1) / (64 * VEC))};
-  float* sums = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + maps_bytes(p, a.B, a.d));
   const bool flags = a.mask || a.reset || a.L % T;
   if (grad)
-    return flags ? launch_grad<BF16, VEC, true, WIDE>(a, c, p, sums, st)
-                 : launch_grad<BF16, VEC, false, WIDE>(a, c, p, sums, st);
+    return flags ? launch_grad<BF16, VEC, true, WIDE>(a, c, p, rest, st)
+                 : launch_grad<BF16, VEC, false, WIDE>(a, c, p, rest, st);
   return flags ? launch<BF16, VEC, true, WIDE>(a, c, p, st)
                : launch<BF16, VEC, false, WIDE>(a, c, p, st);
 }
@@ -905,7 +914,10 @@ hipError_t dispatch(const LruArgs& a, bool grad, bool pairs, hipStream_t st) {
 
 }  // namespace
 
-size_t lru_workspace_bytes(int L, int B, int d) { return maps_bytes(plan(L, B, d, false), B, d); }
+size_t lru_workspace_bytes(int L, int B, int d) {
+  const Plan p = plan(L, B, d, false);
+  return p.chunks == 1 ? 0 : maps_bytes(p, B, d) + sizeof(float) * (size_t)B * d;
+}
 
 size_t lru_grad_workspace_bytes(int L, int B, int d) {
   const Plan p = plan(L, B, d, true);

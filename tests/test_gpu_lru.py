@@ -266,6 +266,24 @@ def test_single_tokens_and_cut_calls(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("marks", [False, True])
+@pytest.mark.parametrize("L,B,d", [(1, 3, 66), (300, 4, 64), (600, 8, 64), (600, 255, 64),
+                                   (5000, 1, 66), (20000, 2, 1000)])
+def test_state_carried_on_in_its_own_memory(L, B, d, marks, dtype):
+    """h_last over h0, in one workgroup a sequence and in chunks (of which there
+    are more than run at a time in the fourth case): the bits of a call that has
+    another place for h_last."""
+    t = dev(inputs(L, B, d, dtype, L + d, marks, marks))
+    want = forward(t)
+    for _ in range(3):
+        h = t["h0"].clone()
+        fw = forward(dict(t, h0=h), out=dict(h_last=h))
+        assert fw["h_last"] is h
+        for n in ("H", "h_last", "states"):
+            assert torch.equal(fw[n], want[n]), n
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
 def test_single_tokens_with_mask_and_reset(dtype):
     L, B, d = 40, 5, 70
     t = inputs(L, B, d, dtype, 12, mask=True, reset=True)
