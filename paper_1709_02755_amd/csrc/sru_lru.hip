@@ -50,12 +50,17 @@ constexpr float kTiny = 1.17549435e-38f;
 constexpr float kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+// At least kTiny; a NaN stays one, which fmaxf would drop (v_maximum3_f32 here).
+__device__ __forceinline__ float at_least_tiny(float x) {
+  return __builtin_elementwise_maximum(x, kTiny);
+}
 
 struct Map {
   float A, B;
 };
 __device__ __forceinline__ float apply(Map m, float h) { return m.A == 0.f ? m.B : fmaf(m.A, h, m.B); }
-// `late` after `early`
+// `late` after `early`.  (A NaN may leave A here, and where the steps' maps are
+// made: a decay that is NaN has entered B as well.)
 __device__ __forceinline__ Map join(Map late, Map early) {
   if (late.A == 0.f) return late;
   return Map{early.A == 0.f ? 0.f : fmaxf(late.A * early.A, kTiny), fmaf(late.A, early.B, late.B)};
@@ -225,7 +230,7 @@ __device__ __forceinline__ float decay_kept(float k, float s) {
 template <bool SERIES>
 __device__ __forceinline__ Decay decay_of(float kept) {
   if constexpr (SERIES) return Decay{1.f - kept, kept * (2.f - kept)};
-  const float p = series(kept), e = fmaxf(exp2_hw(-kLog2e * kept), kTiny);
+  const float p = series(kept), e = at_least_tiny(exp2_hw(-kLog2e * kept));
   const bool small = kept < kSeriesEnd;
   const float w = small ? p : 1.f - e;
   return Decay{small ? 1.f - p : e, w * (2.f - w)};
@@ -544,7 +549,7 @@ __device__ __forceinline__ void grad_maps(const Pack<BF16, VEC> (&x)[T],
       const Decay dc = decay_of<SERIES>(decay_kept<SERIES>(k[v], s));
       // a decay of 1 (no rate, or a gate that is shut) adds nothing, and its
       // root's slope, which has no bound, meets a rate of 0: keep it finite
-      const float q = fmaxf(dc.q, kTiny);
+      const float q = at_least_tiny(dc.q);
       const float rb = __builtin_amdgcn_rsqf(q);  // 1 / beta
       const float xv = x[u].get(v), gx = g * xv;
       const float e = fresh ? g : q * rb * g;

@@ -331,6 +331,88 @@ def test_what_does_not_count_reaches_nothing():
     assert bool(torch.isfinite(f3["H"][:, :2]).all())
 
 
+@pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("rates", ["slow", "fast", "mixed"])
+@pytest.mark.parametrize("reset", [False, True])
+@pytest.mark.parametrize("L,B,d", [(40, 2, 70), (700, 2, 70), (24, 520, 6), (32, 1100, 6)])
+def test_no_number_in_a_gate_or_a_rate(L, B, d, reset, rates, dtype):
+    """A NaN that counts, in r, i or lam: it shows in everything that depends on
+    it, whatever the rates around it, and in nothing else."""
+    t = inputs(L, B, d, dtype, L + d, slow=rates != "fast")
+    b, j, at = 1, 3, L // 2
+    if rates == "mixed":
+        t["lam"][j + 1] = 1.0  # in the same wave
+    first, end = 0, L  # the document that the step belongs to
+    if reset:
+        first, end = L // 4, 3 * L // 4
+        t["reset"] = torch.zeros((L, B), dtype=torch.uint8)
+        t["reset"][[first, end], b] = 1
+    v = dev(t)
+    fw = forward(v)
+    g = backward(v, fw["states"])
+
+    def broken(name, index):
+        w = dict(t, **{name: t[name].clone()})
+        w[name][index] = math.nan
+        w = dev(w)
+        f = forward(w)
+        return f, backward(w, f["states"])
+
+    def agree(name, got, clean, nan):
+        """NaN exactly at `nan`, the clean call's results elsewhere."""
+        got, clean = got.cpu(), clean.cpu()
+        assert torch.equal(torch.isnan(got), nan), name
+        close(name, got.masked_fill(nan, 0), clean.masked_fill(nan, 0).double())
+
+    def no(shape):
+        return torch.zeros(shape, dtype=torch.bool)
+
+    everything = ("H", "dx", "dr", "di")
+    for name in ("r", "i"):
+        f, q = broken(name, (at, b, j))
+        nan = {n: no((L, B, d)) for n in everything}
+        nan["H"][at:end, b, j] = True
+        for n in ("dx", "dr", "di"):
+            nan[n][at, b, j] = True
+        nan["dr"][at + 1:end, b, j] = True  # of a state that is none
+        last, dh0, dlam = no((B, d)), no((B, d)), no(d)
+        last[b, j], dlam[j] = not reset, True
+        if name == "r":  # the gradient of what came before passes its decay
+            nan["dx"][first:at, b, j] = nan["di"][first:at, b, j] = True
+            nan["dr"][first + reset:at, b, j] = True
+            dh0[b, j] = not reset
+        agree("H", f["H"], fw["H"], nan["H"])
+        agree("h_last", f["h_last"], fw["h_last"], last)
+        for n in ("dx", "dr", "di"):
+            agree(name + " " + n, q[n], g[n], nan[n])
+        agree("dh0", q["dh0"], g["dh0"], dh0)
+        agree("dlam", q["dlam"], g["dlam"], dlam)
+
+    f, q = broken("lam", j)
+    fresh = no((L, B)) if t["reset"] is None else t["reset"] != 0
+    nan = no((L, B, d))
+    nan[..., j] = ~fresh
+    agree("H", f["H"], fw["H"], nan)
+    of_lam = no(d)
+    of_lam[j] = True
+    assert bool(torch.isnan(f["h_last"][:, j]).all())
+    agree("dr", q["dr"], g["dr"], nan)
+    agree("dlam", q["dlam"], g["dlam"], of_lam)
+    for n in ("dx", "di"):
+        assert bool(torch.isnan(q[n].cpu()[nan]).all()), n
+        others = no((L, B, d))
+        others[..., j] = True
+        close(n, q[n].cpu().masked_fill(others, 0), g[n].cpu().masked_fill(others, 0).double())
+
+    h = v["h0"].clone()
+    r = v["r"][0].clone()
+    r[b, j] = math.nan
+    y = lm.lru_step(v["x"][0], r, v["i"][0], v["lam"], h, c=C)
+    alone = no((B, d))
+    alone[b, j] = True
+    assert torch.equal(torch.isnan(y).cpu(), alone) and torch.equal(torch.isnan(h).cpu(), alone)
+
+
 def test_extreme_gates():
     """Gates shut and open beyond fp32's range, decays of 0 and of 1."""
     L, B, d = 140, 1, 12
