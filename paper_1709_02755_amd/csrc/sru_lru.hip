@@ -816,9 +816,11 @@ struct Plan {
   bool wide;                      // large workgroups of one channel a lane
   int waves, nseg, each, chunks;  // of a workgroup, segments, those of a chunk, chunks
 };
+// Groups of one channel a lane; d may be any int, for the check of the sizes.
+long long lane_groups(int B, int d) { return B * ((d + 63LL) / 64); }
 Plan plan(int L, int B, int d, bool grad) {
   const int n = (L + T - 1) / T;
-  const long long groups = (long long)B * ((d + 63) / 64);
+  const long long groups = lane_groups(B, d);
   const int wide = grad ? kWideGradWaves : kWideWaves;
   Plan p;
   p.wide = groups < (grad ? kGradMany : kMany) && (groups >= kFew || n <= kWideRounds * wide);
@@ -930,9 +932,7 @@ size_t lru_grad_workspace_bytes(int L, int B, int d) {
 }
 
 long long lru_blocks(int L, int B, int d) {
-  // one channel a lane
-  return (long long)B * ((d + 63) / 64) *
-         std::max(plan(L, B, d, false).chunks, plan(L, B, d, true).chunks);
+  return lane_groups(B, d) * std::max(plan(L, B, d, false).chunks, plan(L, B, d, true).chunks);
 }
 
 hipError_t lru_launch(const LruArgs& a, hipStream_t stream) {

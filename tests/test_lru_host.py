@@ -85,6 +85,21 @@ def test_sizes_that_fit_a_launch():
     assert b(1, 1 << 23, 1) == 0        # 2^23 workgroups
 
 
+@pytest.mark.parametrize("L,B,d", [(1, 1, 2 ** 31 - 1), (8, 1, 2 ** 31 - 63), (1, 1, 2 ** 31 - 65),
+                                   (1, 3, 2 ** 29), (1, 2 ** 22, 64)])
+def test_widths_past_every_launch(L, B, d):
+    """Refused before a launch, also where a width rounded up to whole waves is
+    no int any more."""
+    f, b = sru.lib().sru_lru_forward_workspace_bytes, sru.lib().sru_lru_backward_workspace_bytes
+    assert f(L, B, d) == 0 and b(L, B, d) == 0
+    size = dict(L=L, B=B, d=d)
+    for n in ("x", "r", "i", "H", "dH", "dx", "dr", "di"):
+        size.update({n + "_t": B * d, n + "_b": d})
+    for call, names in ((forward, "xriH"), (backward, ("x", "r", "i", "dH", "dx", "dr", "di"))):
+        kw = {k: v for k, v in size.items() if k in "LBd" or k[:-2] in names}
+        assert call(**kw) == E_SHAPE
+
+
 class Stub:
     def __init__(self):
         self.calls = []
