@@ -87,18 +87,23 @@ def build_sanitized(verbose: bool = False) -> str:
     if not all(os.path.exists(os.path.join(OBJDIR, os.path.basename(p) + ".o"))
                for p in glob.glob(os.path.join(CSRC, "*.hip"))):
         build()
-    apis = [os.path.join(CSRC, n) for n in ("sru_api.hip", "sru_lm_api.hip")]
+    # the C ABI, and the sources whose host code cuts rows and sequences by their sizes
+    names = ("sru_api.hip", "sru_lm_api.hip", "sru_lru.hip", "sru_vocab.hip")
+    srcs = [os.path.join(CSRC, n) for n in names]
     flags = [f if f != "-O3" else "-O1" for f in HIP_FLAGS] + ["-g"]
-    sanitized = []
-    for api in apis:
-        obj = os.path.join(OBJDIR, os.path.basename(api) + ".sanitized.o")
-        cmd = [hipcc(), "-x", "hip", "-c", api, "-o", obj] + flags + SAN_FLAGS
+
+    def compile_sanitized(src):
+        obj = os.path.join(OBJDIR, os.path.basename(src) + ".sanitized.o")
+        cmd = [hipcc(), "-x", "hip", "-c", src, "-o", obj] + flags + SAN_FLAGS
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"sanitized compile failed:\n{r.stdout}\n{r.stderr}")
-        sanitized.append(obj)
+        return obj
+
+    with ThreadPoolExecutor(max_workers=len(srcs)) as ex:
+        sanitized = list(ex.map(compile_sanitized, srcs))
     others = [os.path.join(OBJDIR, os.path.basename(p) + ".o")
-              for p in sorted(glob.glob(os.path.join(CSRC, "*.hip"))) if p not in apis]
+              for p in sorted(glob.glob(os.path.join(CSRC, "*.hip"))) if p not in srcs]
     cmd = ([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-shared-libsan", "-o",
             SAN_LIB] + sanitized + others + SAN_FLAGS)
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -952,7 +952,7 @@ constexpr int kUnroll = 4;
 // 17.9 and 15.9; with alternatives it is as much on the GPU, 14.0 and 18.2, as the
 // launch takes from the host).
 int parts_of(int N, int most) {
-  const int want = (512 + N - 1) / N, p = want < most ? want : most;
+  const int want = (int)((511LL + N) / N), p = want < most ? want : most;
   return p < 1 ? 1 : p > kMaxParts ? kMaxParts : p;
 }
 int row_parts(int N, int V, bool bf16) {

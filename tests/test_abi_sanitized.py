@@ -44,3 +44,19 @@ def test_abi_checks_are_clean_under_asan_and_ubsan(sanitized_lib):
     assert r.returncode == 0, (r.stdout[-3000:], r.stderr[-3000:])
     assert "passed" in r.stdout and "ERROR: AddressSanitizer" not in r.stderr
     assert "runtime error:" not in r.stderr
+
+
+def test_language_model_checks_are_clean_under_asan_and_ubsan(sanitized_lib):
+    """The same of the operators around the layer: their checks, and how rows and
+    sequences of any size are cut."""
+    env = dict(os.environ)
+    env.update(LD_PRELOAD=build.sanitizer_runtime(), SRU_LIBRARY=sanitized_lib,
+               ASAN_OPTIONS="detect_leaks=0:halt_on_error=1:abort_on_error=0",
+               UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-p", "no:cacheprovider"]
+                       + [os.path.join(ROOT, "tests", n) for n in
+                          ("test_lru_host.py", "test_norm_host.py", "test_vocab_host.py")],
+                       env=env, capture_output=True, text=True, timeout=600, cwd=ROOT)
+    assert r.returncode == 0, (r.stdout[-3000:], r.stderr[-3000:])
+    assert "passed" in r.stdout and "ERROR: AddressSanitizer" not in r.stderr
+    assert "runtime error:" not in r.stderr

@@ -116,6 +116,16 @@ def test_workspace_queries():
     assert lib.sru_distill_workspace_bytes(1, 10, 0) == 0
 
 
+def test_rows_of_every_count():
+    """Counts of rows up to the largest int have a cut (the sums of sizes are
+    looked at in the sanitized build)."""
+    lib, most = sru.lib(), 2 ** 31 - 1
+    for N in (most, most - 510, most - 512):
+        for V in (1, 65536, 2 ** 30):
+            assert lib.sru_token_logprobs_workspace_bytes(N, V, 1, 20) == 0  # a row each
+            assert lib.sru_distill_workspace_bytes(N, V, 0) == 0
+
+
 class Stub:
     def __init__(self):
         self.calls = []
