@@ -133,6 +133,8 @@ def token_logprobs(logits, tokens, top=0, temperature=1.0, out=None, ws=None):
     be strided; logits of -inf are tokens that are not possible."""
     code, N, V, dv, ld = _logits(logits, temperature)
     _req(tokens, "tokens", (N,), dtype=_I64, device=dv)
+    if not 0 <= top <= MAX_TOP:
+        raise ValueError(f"top must be 0 .. {MAX_TOP}, got {top}")
     o = dict(logprob=_out(out, "logprob", (N,), _F32, logits),
              entropy=_out(out, "entropy", (N,), _F32, logits),
              stats=_out(out, "stats", (N, 2), _F32, logits),

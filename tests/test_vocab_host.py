@@ -197,3 +197,11 @@ def test_binding_checks_every_tensor(stub):
 def test_host_tensors_are_refused():
     with pytest.raises(ValueError, match="GPU"):
         lm.token_logprobs(torch.zeros((N, V)), torch.zeros(N, dtype=torch.int64))
+
+
+@pytest.mark.parametrize("top", [-1, 65, 1 << 32, 1 << 40])
+def test_alternatives_out_of_range(top, stub):
+    """Refused before anything of their size is allocated."""
+    with pytest.raises(ValueError, match="top"):
+        lm.token_logprobs(torch.zeros((N, V)), torch.zeros(N, dtype=torch.int64), top=top)
+    assert stub.calls == []
