@@ -20,6 +20,7 @@ DTYPE_FP32, DTYPE_BF16 = 0, 1
 MAX_TOP, MAX_TEACHER = 64, 1024
 GATE_SILU, GATE_SIGMOID = 0, 1
 LRU_STEPS = 8
+_INT_MAX = (1 << 31) - 1  # sizes are ints in the library; ctypes would cut larger ones
 
 _CODES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
 
@@ -46,6 +47,10 @@ def _dtype(t, name):
     if t.dtype not in _CODES:
         raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
     return _CODES[t.dtype]
+
+
+def _too_large(t, name):
+    return ValueError(f"{name} is too large: {tuple(t.shape)}")
 
 
 def _here(t, name):
@@ -110,6 +115,8 @@ def _logits(logits, temperature):
     if not 0.0 < temperature < float("inf"):
         raise ValueError(f"temperature must be positive and finite, got {temperature}")
     N, V = logits.shape
+    if N > _INT_MAX or V > _INT_MAX:
+        raise _too_large(logits, "logits")
     return code, N, V, dv, _pitch(logits, "logits", (N, V), logits.dtype, dv)
 
 
@@ -189,6 +196,8 @@ def _teacher(teacher_ids, teacher_logits, N, dv):
     if teacher_logits.dim() != 2:
         raise ValueError("teacher_logits must be a 2-d tensor [N, K]")
     K = teacher_logits.shape[1]
+    if K > _INT_MAX:
+        raise _too_large(teacher_logits, "teacher_logits")
     _req(teacher_ids, "teacher_ids", (N, K), dtype=_I64, device=dv)
     _req(teacher_logits, "teacher_logits", (N, K), dtype=teacher_logits.dtype, device=dv)
     return code, K
@@ -303,7 +312,10 @@ def _norm_inputs(x, y, z, w_post, scale, w_pre):
     for n, w in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
         if w is not None and not _plain(w, (d,), _F32, dv):
             _req(w, n, (d,), device=dv)
-    return x.numel() // d if d else 0, d, act, code, res, dv, pitch
+    M = x.numel() // d if d else 0
+    if M > _INT_MAX or d > _INT_MAX:
+        raise _too_large(x, "x")
+    return M, d, act, code, res, dv, pitch
 
 
 def _row_out(out, name, like):
@@ -398,6 +410,8 @@ def _lru_inputs(x, r, i, lam, mask, reset):
     dv = _here(x, "x")
     shape = x.shape
     L, B, d = shape
+    if L > _INT_MAX or B > _INT_MAX or d > _INT_MAX:
+        raise _too_large(x, "x")
     steps = (_seq(x, "x", shape, x.dtype, dv), _seq(r, "r", shape, x.dtype, dv),
              _seq(i, "i", shape, x.dtype, dv))
     _req(lam, "lam", (d,), device=dv)
@@ -487,6 +501,8 @@ def lru_step(x, r, i, lam, h, c=8.0, out=None, mask=None, reset=None):
         raise ValueError("x must be a 2-d tensor [B, d]")
     dv, dt, shape = _here(x, "x"), x.dtype, x.shape
     B, d = shape
+    if B > _INT_MAX or d > _INT_MAX:
+        raise _too_large(x, "x")
     fast = x.stride(1) == 1
     for n, t in (("r", r), ("i", i)):
         fast = (fast and t.__class__ is torch.Tensor and t.dtype is dt and t.shape == shape

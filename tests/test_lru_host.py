@@ -182,3 +182,20 @@ def test_host_tensors_are_refused():
     x = torch.zeros((2, 1, 8))
     with pytest.raises(ValueError, match="GPU"):
         lm.lru_forward(x, x, x, torch.zeros(8))
+
+
+@pytest.mark.parametrize("shape", [((1 << 32) + 5, 1, 1), (1, (1 << 32) + 5, 1),
+                                   (1, 1, (1 << 32) + 5), (1 << 31, 1, 1)])
+def test_sizes_past_32_bits_are_refused(shape, stub):
+    """By the binding: the library's sizes are ints.  (Tensors without memory.)"""
+    L, B, d = shape
+    x, lam = torch.empty(shape, device="meta"), torch.empty(d, device="meta")
+    states = torch.empty((-(-L // 8), B, d), device="meta")
+    with pytest.raises(ValueError, match="large"):
+        lm.lru_forward(x, x, x, lam)
+    with pytest.raises(ValueError, match="large"):
+        lm.lru_backward(x, x, x, lam, states, x)
+    if L == 1:
+        with pytest.raises(ValueError, match="large"):
+            lm.lru_step(x[0], x[0], x[0], lam, torch.empty((B, d), device="meta"))
+    assert stub.calls == []

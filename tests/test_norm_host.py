@@ -146,3 +146,16 @@ def test_binding(stub):
 def test_host_tensors_are_refused():
     with pytest.raises(ValueError, match="GPU"):
         lm.residual_norm_forward(torch.zeros((2, 8)), w_pre=torch.zeros(8))
+
+
+@pytest.mark.parametrize("shape", [((1 << 32) + 5, 1), (1 << 31, 1), (1 << 16, 1 << 16, 2),
+                                   (1, (1 << 32) + 5)])
+def test_sizes_past_32_bits_are_refused(shape, stub):
+    """By the binding: the library's sizes are ints.  (Tensors without memory.)"""
+    x, w = torch.empty(shape, device="meta"), torch.empty(shape[-1], device="meta")
+    with pytest.raises(ValueError, match="large"):
+        lm.residual_norm_forward(x, x, w_pre=w)
+    with pytest.raises(ValueError, match="large"):
+        lm.residual_norm_backward(x, x, torch.empty((*shape[:-1], 2), device="meta"), x, x,
+                                  w_pre=w)
+    assert stub.calls == []

@@ -205,3 +205,29 @@ def test_alternatives_out_of_range(top, stub):
     with pytest.raises(ValueError, match="top"):
         lm.token_logprobs(torch.zeros((N, V)), torch.zeros(N, dtype=torch.int64), top=top)
     assert stub.calls == []
+
+
+BIG = (1 << 32) + 5  # cut to 32 bits it is 5
+
+
+def test_sizes_past_32_bits_are_refused(stub):
+    """By the binding: the library's sizes are ints.  (Tensors without memory.)"""
+    def z(n, v):
+        return torch.empty((n, v), device="meta")
+
+    def i64(*shape):
+        return torch.empty(shape, dtype=torch.int64, device="meta")
+
+    for n, v in ((BIG, 1), (1, BIG), (1 << 31, 1)):
+        f = torch.empty(n, device="meta")
+        fw = dict(stats=z(n, 2), entropy=f, top_ids=None)
+        for call in (lambda: lm.token_logprobs(z(n, v), i64(n)),
+                     lambda: lm.token_logprobs_backward(z(n, v), i64(n), fw, f),
+                     lambda: lm.distill_forward(z(n, v), i64(n, 2), z(n, 2)),
+                     lambda: lm.distill_backward(z(n, v), i64(n, 2), z(n, 2), fw["stats"], f),
+                     lambda: lm.distill_forward_backward(z(n, v), i64(n, 2), z(n, 2), f)):
+            with pytest.raises(ValueError, match="large"):
+                call()
+    with pytest.raises(ValueError, match="large"):
+        lm.distill_forward(z(3, 10), i64(3, BIG), z(3, BIG))
+    assert stub.calls == []
