@@ -340,7 +340,7 @@ SRU_API int sru_scan_backward(const float* U, const float* X, const float* C, co
 typedef enum { SRU_DTYPE_FP32 = 0, SRU_DTYPE_BF16 = 1 } sru_dtype;
 
 /* Vocabulary rows: logits [N, V], row pitch ld >= V elements, columns
- * contiguous, at a temperature T > 0 (finite):
+ * contiguous, at a temperature T > 0 (finite, and so is log2(e) / T):
  *   m = max_j z_j,  S = sum_j exp((z_j - m) / T),
  *   log p_j = (z_j - m) / T - log S
  * stats [N, 2] holds (m, S) for the gradient calls.  Logits may be -inf (a

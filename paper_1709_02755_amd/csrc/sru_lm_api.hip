@@ -44,7 +44,9 @@ int check_rows(const void* z, long long ld, int dtype, int N, int V, float tempe
   if (!valid_dtype(dtype)) return SRU_E_FLAG;
   // a column past a row's end is told by its sign
   if (N <= 0 || V <= 0 || V > INT_MAX / 2 || ld < V || ld > kMaxElems / N) return SRU_E_SHAPE;
-  if (!std::isfinite(temperature) || !(temperature > 0.f) || !std::isfinite(1.f / temperature))
+  // log2(e) / T, in which the kernels count, is finite as well
+  if (!std::isfinite(temperature) || !(temperature > 0.f) ||
+      !std::isfinite(1.44269504088896341f / temperature))
     return SRU_E_SHAPE;
   if (!z) return SRU_E_NULLPTR;
   if (!aligned(z, elem_size(dtype))) return SRU_E_ALIGN;

@@ -65,6 +65,12 @@ def test_rows_are_checked_by_every_call(kw, want):
         assert distill(name, **kw) == want
 
 
+@pytest.mark.parametrize("T", [4e-39, 3.5e-39, 3e-39])
+def test_temperatures_whose_exponents_are_no_numbers(T):
+    """1 / T is finite here and log2(e) / T, which the kernels use, is not."""
+    test_rows_are_checked_by_every_call(dict(T=T), E_SHAPE)
+
+
 @pytest.mark.parametrize("kw,want", [
     (dict(top=65), E_SHAPE), (dict(top=-1), E_SHAPE), (dict(top=8, V=7, ld=7), E_SHAPE),
     (dict(tok=None), E_NULL), (dict(lp=None), E_NULL), (dict(ent=None), E_NULL),
