@@ -290,9 +290,9 @@ def _row_pitch(t, name, shape, dtype, device):
     return d if ld is None else ld
 
 
-def _norm_inputs(x, y, z, w_post, scale, w_pre):
-    """Checked inputs: M, d, activation type, its code, residual code, device,
-    and the pitches of x, y and z."""
+def _norm_inputs(x, y, z, w_post, scale, w_pre, dtype=None):
+    """Checked inputs: M, d, activation type (dtype, where there is no y to have
+    it), its code, residual code, device, and the pitches of x, y and z."""
     res = _dtype(x, "x")
     if x.dim() < 1:
         raise ValueError("x must have a last dimension")
@@ -302,11 +302,12 @@ def _norm_inputs(x, y, z, w_post, scale, w_pre):
     if y is None:
         if w_pre is None or w_post is not None or z is not None or scale is not None:
             raise ValueError("without y there is only the norm of x: give w_pre alone")
-        act, code = x.dtype, res
+        act = x.dtype if dtype is None else dtype
+        code = _CODES.get(act)
     else:
         act, code = y.dtype if isinstance(y, torch.Tensor) else None, _dtype(y, "y")
-        if x.dtype != act and x.dtype != _F32:
-            raise ValueError(f"x must be {act} or float32, got {x.dtype}")
+    if x.dtype != act and (x.dtype != _F32 or code is None):
+        raise ValueError(f"x must be {act} or float32 beside bfloat16, got {x.dtype}")
     pitch = (_row_pitch(x, "x", shape, x.dtype, dv), _row_pitch(y, "y", shape, act, dv),
              _row_pitch(z, "z", shape, act, dv))
     for n, w in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
@@ -318,17 +319,20 @@ def _norm_inputs(x, y, z, w_post, scale, w_pre):
     return M, d, act, code, res, dv, pitch
 
 
-def _row_out(out, name, like):
-    """(out[name] or a new tensor, of the shape and type of `like`; its row
-    pitch)."""
+def _row_out(out, name, like, dtype=None):
+    """(out[name] or a new tensor, of the shape and type of `like` (or of type
+    dtype); its row pitch)."""
     t = None if out is None else out.get(name)
-    if t is None:
-        return _new_like(like), like.shape[-1]
-    return t, _row_pitch(t, name, like.shape, like.dtype, like.device)
+    if dtype is None:
+        dtype = like.dtype
+    if t is not None:
+        return t, _row_pitch(t, name, like.shape, dtype, like.device)
+    t = _new_like(like) if dtype is like.dtype else like.new_empty(like.shape, dtype=dtype)
+    return t, like.shape[-1]
 
 
 def residual_norm_forward(x, y=None, w_post=None, z=None, scale=None, w_pre=None,
-                          gate=GATE_SILU, eps=1e-6, out=None):
+                          gate=GATE_SILU, eps=1e-6, out=None, dtype=None):
     """Between two blocks: dict(x_out, o, rstd) with
 
         x_out = x + scale * (y rstd(y) w_post) * gate(z)
@@ -338,14 +342,17 @@ def residual_norm_forward(x, y=None, w_post=None, z=None, scale=None, w_pre=None
     output, z the gate's input (z sigma(z), or sigma(z) with GATE_SIGMOID);
     w_post, scale and w_pre are float32 [d].  Each of w_post, z, scale and w_pre
     may be None (no norm of y, no gate, scale 1, no o); without y, o is the norm
-    of x.  x may be float32 beside bfloat16 activations.  Rows may be strided
-    (slices of a projection).  out may hold x_out (x itself), o and rstd."""
-    M, d, act, code, res, dv, (ldx, ldy, ldz) = _norm_inputs(x, y, z, w_post, scale, w_pre)
+    of x.  x may be float32 beside bfloat16 activations; the type of o is y's, or
+    without y `dtype` (None: x's).  Rows may be strided (slices of a projection).
+    out may hold x_out (x itself), o and rstd."""
+    M, d, act, code, res, dv, (ldx, ldy, ldz) = _norm_inputs(x, y, z, w_post, scale, w_pre, dtype)
+    if dtype is not None and dtype != act:
+        raise ValueError(f"y is {act}, and so is o: not {dtype}")
     x_out, o, ldxo, ldo = None, None, 0, 0
     if y is not None:
         x_out, ldxo = _row_out(out, "x_out", x)
     if w_pre is not None:
-        o, ldo = _row_out(out, "o", x if y is None else y)
+        o, ldo = _row_out(out, "o", x if y is None else y, act)
     rstd = _out(out, "rstd", (*x.shape[:-1], 2), _F32, x)
     st = sru.lib().sru_residual_norm_forward(M, d, code, res, gate, eps, _ptr(x), ldx, _ptr(y),
                                              ldy, _ptr(z), ldz, _ptr(w_post), _ptr(scale),
@@ -358,10 +365,12 @@ def residual_norm_forward(x, y=None, w_post=None, z=None, scale=None, w_pre=None
 def residual_norm_backward(x, y, rstd, dx_out=None, do=None, w_post=None, z=None, scale=None,
                            w_pre=None, gate=GATE_SILU, eps=1e-6, out=None, ws=None):
     """Gradients of residual_norm_forward, given its inputs, its rstd (which
-    holds eps) and the gradients of x_out and o (None: zeros): dict(dx, dy, dz,
-    dw_post, dscale, dw_pre), None where the input was.  out may hold any of
-    them (dx may be dx_out itself, dy and dz slices of a larger tensor)."""
-    M, d, act, code, res, dv, (ldx, ldy, ldz) = _norm_inputs(x, y, z, w_post, scale, w_pre)
+    holds eps) and the gradients of x_out and o (None: zeros; do has the type of
+    o): dict(dx, dy, dz, dw_post, dscale, dw_pre), None where the input was.  out
+    may hold any of them (dx may be dx_out itself, dy and dz slices of a larger
+    tensor)."""
+    M, d, act, code, res, dv, (ldx, ldy, ldz) = _norm_inputs(
+        x, y, z, w_post, scale, w_pre, do.dtype if isinstance(do, torch.Tensor) else None)
     shape = x.shape
     _req(rstd, "rstd", tuple(shape[:-1]) + (2,), device=dv)
     lddxo = _row_pitch(dx_out, "dx_out", shape, x.dtype, dv)

@@ -180,6 +180,23 @@ def test_parts_left_out(drop, act, res):
         check(inputs(6, d, act, res, 2, drop), lm.GATE_SILU)
 
 
+@pytest.mark.parametrize("M,d", [(5, 40), (3, 1024), (4, 1277), (2, 6001)])
+def test_norm_alone_beside_a_full_precision_residual(M, d):
+    """What a bfloat16 model's first block reads of a float32 residual."""
+    t = inputs(M, d, B16, F32, d, ("y", "z", "w_post", "scale"))
+    _, o, ref = plain(t, lm.GATE_SILU)
+    mag = magnitudes(t, lm.GATE_SILU)
+    v = dev(t)
+    fw = lm.residual_norm_forward(v["x"], w_pre=v["w_pre"], eps=EPS, dtype=B16)
+    g = lm.residual_norm_backward(v["x"], None, fw["rstd"], v["dx_out"], v["do"], w_pre=v["w_pre"],
+                                  eps=EPS)
+    torch.cuda.synchronize()
+    assert fw["o"].dtype == B16 and g["dx"].dtype == F32
+    close("o", fw["o"], o, mag["o"])
+    close("dx", g["dx"], ref["x"], mag["x"])
+    close("dw_pre", g["dw_pre"], ref["w_pre"], mag["w_pre"])
+
+
 @pytest.mark.parametrize("d", [64, 1024])
 def test_many_rows(d):
     """More rows than the gradient's workgroups take at a time."""

@@ -159,3 +159,33 @@ def test_sizes_past_32_bits_are_refused(shape, stub):
         lm.residual_norm_backward(x, x, torch.empty((*shape[:-1], 2), device="meta"), x, x,
                                   w_pre=w)
     assert stub.calls == []
+
+
+def test_first_norm_of_a_full_precision_residual(stub):
+    """The norm of x alone, o in bfloat16 beside a float32 x, as the C call has it."""
+    M, d = 3, 8
+    x, y, w = torch.zeros((M, d)), torch.zeros((M, d), dtype=B16), torch.zeros(d)
+    fw = lm.residual_norm_forward(x, w_pre=w, dtype=B16)
+    assert fw["o"].dtype == B16 and fw["x_out"] is None
+    assert stub.calls[-1][1][2:4] == (lm.DTYPE_BF16, lm.DTYPE_FP32)
+    assert lm.residual_norm_forward(x, w_pre=w, dtype=B16, out=dict(o=y))["o"] is y
+    assert lm.residual_norm_forward(y, w_pre=w, dtype=B16)["o"].dtype == B16
+    assert lm.residual_norm_forward(x, y, w_pre=w, dtype=B16)["o"].dtype == B16
+    assert lm.residual_norm_forward(x, w_pre=w)["o"].dtype == torch.float32
+    g = lm.residual_norm_backward(x, None, fw["rstd"], x, y, w_pre=w)
+    assert g["dx"].dtype == torch.float32
+    assert stub.calls[-1][1][2:4] == (lm.DTYPE_BF16, lm.DTYPE_FP32)
+    assert lm.residual_norm_backward(x, None, fw["rstd"], x, w_pre=w)["dx"].dtype == torch.float32
+    reached = len(stub.calls)
+    bad = [
+        lambda: lm.residual_norm_forward(y, w_pre=w, dtype=torch.float32),
+        lambda: lm.residual_norm_forward(x, w_pre=w, dtype=torch.half),
+        lambda: lm.residual_norm_forward(x, y, w_pre=w, dtype=torch.float32),
+        lambda: lm.residual_norm_forward(x, w_pre=w, dtype=B16, out=dict(o=x)),
+        lambda: lm.residual_norm_backward(y, None, fw["rstd"], y, x, w_pre=w),
+        lambda: lm.residual_norm_backward(x, None, fw["rstd"], y, y, w_pre=w),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+        assert len(stub.calls) == reached, i
