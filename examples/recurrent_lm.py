@@ -181,6 +181,12 @@ class Source:
         at = s[:-1].reshape(-1)
         return s[:-1].contiguous(), s[1:].contiguous(), self.ids[at], self.logits[at]
 
+    def logprobs(self, targets, ids, logits):
+        """The source's own log probabilities of targets [N], given batch's ids and
+        logits; a token that is among the successors twice has both chances."""
+        each = logits.log_softmax(1).masked_fill(ids != targets[:, None], -float("inf"))
+        return each.logsumexp(1)
+
 
 def main():
     a = argparse.ArgumentParser()
@@ -213,9 +219,9 @@ def main():
             print(f"step {n:4d} {kind:8s} loss {float(loss):.4f}", flush=True)
     tokens, targets, ids, logits = source.batch(a.length, a.streams)
     r = model.score(tokens, targets)
-    best = lm.token_logprobs(logits, (ids == targets.reshape(-1, 1)).to(torch.int64).argmax(1))
+    best = source.logprobs(targets.reshape(-1), ids, logits)
     print(f"held out: {-float(r['logprob'].mean()):.4f} nats per token "
-          f"(the source itself: {-float(best['logprob'].mean()):.4f}), "
+          f"(the source itself: {-float(best.mean()):.4f}), "
           f"entropy {float(r['entropy'].mean()):.4f}")
     first = torch.zeros(4, dtype=torch.int64, device=dev)
     said, logps = model.generate(first, 12, model.new_state(4))
