@@ -430,6 +430,66 @@ def test_extreme_gates():
         assert bool(torch.isfinite(n).all())
 
 
+def closed_form(t):
+    """The gradients by their formulas in 64 bits, and the magnitudes of what each
+    is made of (the same sums of absolute values)."""
+    v = {n: t[n].double() for n in ("x", "r", "i", "lam", "h0", "dH", "dh_last")}
+    L = v["x"].shape[0]
+    s, not_s, g, not_g = (torch.sigmoid(w) for w in (v["r"], -v["r"], v["i"], -v["i"]))
+    k = C * torch.nn.functional.softplus(v["lam"])
+    a, beta = torch.exp(-k * s), torch.sqrt(-torch.expm1(-2 * k * s))
+
+    def through_time(h, x, G, dH, sign):
+        befores, Gs = [], [None] * L
+        for n in range(L):
+            befores.append(h)
+            h = a[n] * h + beta[n] * g[n] * x[n]
+        for n in reversed(range(L)):
+            Gs[n] = dH[n] + G
+            G = a[n] * Gs[n]
+        G_all = torch.stack(Gs)
+        dla = G_all * a * (torch.stack(befores) + sign * a * g * x / beta)
+        return dict(dx=G_all * beta * g, di=G_all * beta * x * g * not_g,
+                    dr=sign * k * dla * s * not_s, dh0=G,
+                    dlam=sign * C * torch.sigmoid(v["lam"]) * (dla * s).sum((0, 1))), G_all
+
+    ref, _ = through_time(v["h0"], v["x"], v["dh_last"], v["dH"], -1.0)
+    mag, G = through_time(*(v[n].abs() for n in ("h0", "x", "dh_last", "dH")), 1.0)
+    return ref, mag, G, g * v["x"].abs()
+
+
+def test_gradients_of_extreme_gates():
+    """The same gates and decays: the gradients are what the formulas say, also
+    where 1 / beta is huge and meets a rate near 0.
+
+    Tolerances: 1e-5 of the largest magnitude in the channel, as above, and what
+    fp32 cannot hold: 1 - a^2 is kept at 2^-126 or more and so its root at 2^-63 =
+    1.1e-19, which dx, di, dr and the terms of dlam depend on by a factor of G (1 +
+    g x) at most; 1e-18 of these covers it."""
+    L, B, d = 140, 2, 12
+    t = inputs(L, B, d, F32, 12)
+    t["lam"] = torch.tensor([-100.0, -30.0, -9.0, 0.0, 5.0, 40.0] * 2)
+    t["r"][:, :, 6:] = 120.0
+    t["r"][::2, :, :3] = -120.0
+    t["i"][::3] = -150.0
+    ref, mag, G, gx = closed_form(t)
+    tiny = 1e-18 * (G * (1 + gx)).amax(0)
+    tol = {n: 1e-5 * mag[n].amax(0) + tiny for n in ("dx", "di", "dr")}
+    tol["dh0"] = 1e-5 * G.amax(0)
+    tol["dlam"] = 1e-5 * mag["dlam"] + 1e-18 * (G * (1 + gx)).sum((0, 1))
+    # all but the least rate's gradients stand out from their tolerances
+    for n in ("dx", "di"):
+        assert bool((ref[n].abs().amax(0) > 1000 * tol[n])[:, [1, 2, 3, 4, 5, 7, 8]].all()), n
+    assert bool((ref["dr"].abs().amax(0) > 1000 * tol["dr"])[:, 1:6].all())
+    assert bool((ref["dlam"].abs() > 10 * tol["dlam"])[[1, 2, 3, 4, 5, 7, 8]].all())
+    v = dev(t)
+    got = backward(v, forward(v)["states"])
+    torch.cuda.synchronize()
+    for n in tol:
+        err = (got[n].cpu().double() - ref[n]).abs()
+        assert bool((err <= tol[n]).all()), (n, float((err / tol[n]).max()))
+
+
 def test_gradient_against_differences():
     t = inputs(19, 2, 6, F32, 13, True, True, slow=False)
     d = dev(t)
