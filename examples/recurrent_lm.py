@@ -2,12 +2,14 @@
 distilled from a teacher's best tokens, scored on held-out text, and run token
 by token.
 
-    python examples/recurrent_lm.py [--steps 200] [--width 256] [--vocab 2048]
+    python examples/recurrent_lm.py [--steps 200] [--width 256] [--vocab 2048] [--bf16]
 
 A block is norm -> one projection to (x, r, i, z) -> gated linear recurrence over
 (x, r, i) -> norm, gate by z and scaled residual.  The call that ends a block
 also makes the next block's normed input, so nothing else runs between the
-products.  Text and teacher are synthetic: a random Markov chain writes the
+products.  With --bf16 the activations between the products are bfloat16, beside a
+float32 residual; the library's products take and give float32 (and round their
+operands), so theirs are converted.  Text and teacher are synthetic: a random Markov chain writes the
 documents, which are packed one after the other (token 0 starts each), and its
 transition logits are the teacher's.
 """
@@ -29,8 +31,10 @@ class RecurrentLM:
     """Parameters by name in `self.p`; gradients by the same names from
     `backward`."""
 
-    def __init__(self, vocab, width, blocks, device, gemm_dtype=sru.GEMM_BF16, seed=0):
+    def __init__(self, vocab, width, blocks, device, gemm_dtype=sru.GEMM_BF16, seed=0,
+                 act=torch.float32):
         g = torch.Generator().manual_seed(seed)
+        self.act = act
         self.vocab, self.width, self.blocks, self.gemm = vocab, width, blocks, gemm_dtype
 
         def normal(*shape, std):
@@ -59,12 +63,13 @@ class RecurrentLM:
         p, (L, B), d = self.p, tokens.shape, self.width
         reset = (tokens == 0).to(torch.uint8)
         x = p["embed"][tokens]
-        o = lm.residual_norm_forward(x, w_pre=p["pre0"])
+        o = lm.residual_norm_forward(x, w_pre=p["pre0"], dtype=self.act)
         saved = dict(tokens=tokens, reset=reset, x0=x, rstd0=o["rstd"], blocks=[])
         o = o["o"]
         for n in range(self.blocks):
-            u = sru.gemm(sru.OP_NT, o.view(L * B, d), p[f"proj{n}"], L * B, 4 * d, d, self.gemm)
-            u = u.view(L, B, 4, d)
+            o = o.view(L * B, d).float()
+            u = sru.gemm(sru.OP_NT, o, p[f"proj{n}"], L * B, 4 * d, d, self.gemm)
+            u = u.view(L, B, 4, d).to(self.act)
             f = lm.lru_forward(u[:, :, 0], u[:, :, 1], u[:, :, 2], p[f"lam{n}"],
                                h0=None if state is None else state[n], reset=reset,
                                keep_states=keep)
@@ -76,33 +81,34 @@ class RecurrentLM:
                 saved["blocks"].append(dict(o=o, u=u, x=x, H=f["H"], states=f["states"],
                                             rstd=e["rstd"]))
             x, o = e["x_out"], e["o"]
-        saved["o"] = o
-        logits = sru.gemm(sru.OP_NT, o.view(L * B, d), p["head"], L * B, self.vocab, d, self.gemm)
-        return logits, saved
+        saved["o"] = o = o.view(L * B, d).float()
+        logits = sru.gemm(sru.OP_NT, o, p["head"], L * B, self.vocab, d, self.gemm)
+        return logits.to(self.act), saved
 
     def backward(self, saved, dlogits):
         """Gradients of the parameters."""
         p, d, V = self.p, self.width, self.vocab
         L, B = saved["tokens"].shape
-        N, g = L * B, {}
-        g["head"] = sru.gemm(sru.OP_TN, dlogits, saved["o"].view(N, d), V, d, N, self.gemm)
+        N, g, dlogits = L * B, {}, dlogits.float()
+        g["head"] = sru.gemm(sru.OP_TN, dlogits, saved["o"], V, d, N, self.gemm)
         do = sru.gemm(sru.OP_NN, dlogits, p["head"], N, d, V, self.gemm).view(L, B, d)
         dx = None
         for n in reversed(range(self.blocks)):
             s = saved["blocks"][n]
             du = torch.empty_like(s["u"])
-            e = lm.residual_norm_backward(s["x"], s["H"], s["rstd"], dx, do, p[f"post{n}"],
-                                          s["u"][:, :, 3], p[f"scale{n}"], p[f"pre{n + 1}"],
-                                          out=dict(dz=du[:, :, 3]))
+            e = lm.residual_norm_backward(s["x"], s["H"], s["rstd"], dx, do.to(self.act),
+                                          p[f"post{n}"], s["u"][:, :, 3], p[f"scale{n}"],
+                                          p[f"pre{n + 1}"], out=dict(dz=du[:, :, 3]))
             f = lm.lru_backward(s["u"][:, :, 0], s["u"][:, :, 1], s["u"][:, :, 2], p[f"lam{n}"],
                                 s["states"], e["dy"], reset=saved["reset"], want_dh0=False,
                                 out=dict(dx=du[:, :, 0], dr=du[:, :, 1], di=du[:, :, 2]))
             g[f"post{n}"], g[f"scale{n}"], g[f"pre{n + 1}"] = e["dw_post"], e["dscale"], e["dw_pre"]
-            g[f"lam{n}"], du = f["dlam"], du.view(N, 4 * d)
-            g[f"proj{n}"] = sru.gemm(sru.OP_TN, du, s["o"].view(N, d), 4 * d, d, N, self.gemm)
+            g[f"lam{n}"], du = f["dlam"], du.view(N, 4 * d).float()
+            g[f"proj{n}"] = sru.gemm(sru.OP_TN, du, s["o"], 4 * d, d, N, self.gemm)
             do = sru.gemm(sru.OP_NN, du, p[f"proj{n}"], N, d, 4 * d, self.gemm).view(L, B, d)
             dx = e["dx"]
-        e = lm.residual_norm_backward(saved["x0"], None, saved["rstd0"], dx, do, w_pre=p["pre0"])
+        e = lm.residual_norm_backward(saved["x0"], None, saved["rstd0"], dx, do.to(self.act),
+                                      w_pre=p["pre0"])
         g["pre0"] = e["dw_pre"]
         g["embed"] = torch.zeros_like(p["embed"])
         g["embed"].index_put_((saved["tokens"].reshape(-1),), e["dx"].view(N, d), accumulate=True)
@@ -114,14 +120,15 @@ class RecurrentLM:
         p, B, d = self.p, tokens.shape[0], self.width
         reset = (tokens == 0).to(torch.uint8)
         x = p["embed"][tokens]
-        o = lm.residual_norm_forward(x, w_pre=p["pre0"])["o"]
+        o = lm.residual_norm_forward(x, w_pre=p["pre0"], dtype=self.act)["o"]
         for n in range(self.blocks):
-            u = sru.gemm(sru.OP_NT, o, p[f"proj{n}"], B, 4 * d, d, self.gemm).view(B, 4, d)
+            u = sru.gemm(sru.OP_NT, o.float(), p[f"proj{n}"], B, 4 * d, d, self.gemm)
+            u = u.view(B, 4, d).to(self.act)
             h = lm.lru_step(u[:, 0], u[:, 1], u[:, 2], p[f"lam{n}"], state[n], reset=reset)
             e = lm.residual_norm_forward(x, h, p[f"post{n}"], u[:, 3], p[f"scale{n}"],
                                          p[f"pre{n + 1}"])
             x, o = e["x_out"], e["o"]
-        return sru.gemm(sru.OP_NT, o, p["head"], B, self.vocab, d, self.gemm)
+        return sru.gemm(sru.OP_NT, o.float(), p["head"], B, self.vocab, d, self.gemm).to(self.act)
 
     def distill(self, tokens, teacher_ids, teacher_logits, temperature=1.0):
         """Mean loss against the teacher's entries [L * B, K], and gradients."""
@@ -196,9 +203,11 @@ def main():
     a.add_argument("--blocks", type=int, default=2)
     a.add_argument("--length", type=int, default=128)
     a.add_argument("--streams", type=int, default=32)
+    a.add_argument("--bf16", action="store_true")
     a = a.parse_args()
     dev = torch.device("cuda:0")
-    model = RecurrentLM(a.vocab, a.width, a.blocks, dev)
+    model = RecurrentLM(a.vocab, a.width, a.blocks, dev,
+                        act=torch.bfloat16 if a.bf16 else torch.float32)
     source = Source(a.vocab, 16, dev)
     opt = torch.optim.Adam(model.p.values(), lr=3e-3)
 

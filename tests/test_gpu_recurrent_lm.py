@@ -78,6 +78,34 @@ def test_gradients_and_loss(width, vocab, L, B):
         assert far(grads[n], ref[n]) <= TOL, n
 
 
+# With bfloat16 activations every tensor between the operators is rounded, by at
+# most 2^-8 of its values: o, u and H of two blocks and the logits forward, dlogits
+# and do, dy and du of two blocks back, 14 of them; times the 5 of above.
+TOL_BF16 = 14 * 5 * 2.0 ** -8
+
+
+@pytest.mark.parametrize("width,vocab,L,B", [(64, 200, 9, 3), (40, 77, 70, 2)])
+def test_gradients_and_loss_with_bfloat16_activations(width, vocab, L, B):
+    dev = torch.device("cuda:0")
+    m = example.RecurrentLM(vocab, width, 2, dev, gemm_dtype=sru.GEMM_FP32, act=torch.bfloat16)
+    tokens, targets, ids, tl = example.Source(vocab, 5, dev).batch(L, B)
+    p = {n: t.double().cpu().requires_grad_() for n, t in m.p.items()}
+    logp = plain(p, tokens.cpu(), 2).log_softmax(1)
+    loss = -logp.gather(1, targets.cpu().reshape(-1, 1)).mean()
+    q = tl.double().cpu().log_softmax(1)
+    kl = (q.exp() * (q - logp.gather(1, ids.cpu()))).sum() / (L * B)
+    for of, (got, grads) in ((loss, m.fit(tokens, targets)), (kl, m.distill(tokens, ids, tl))):
+        ref = dict(zip(p, torch.autograd.grad(of, p.values(), retain_graph=True)))
+        assert abs(float(got) - of.item()) <= TOL_BF16 * of.item()
+        for n in p:
+            assert far(grads[n], ref[n]) <= TOL_BF16, n
+    state = m.new_state(B)
+    steps = torch.stack([m.step(tokens[t], state) for t in range(L)])
+    assert steps.dtype == torch.bfloat16
+    whole = m.forward(tokens)[0].view(L, B, vocab)
+    assert far(steps, whole.double().cpu()) <= TOL_BF16
+
+
 def test_one_token_at_a_time_and_in_pieces():
     dev, L, B, V = torch.device("cuda:0"), 37, 5, 130
     m = example.RecurrentLM(V, 96, 2, dev, gemm_dtype=sru.GEMM_FP32)
