@@ -339,7 +339,7 @@ SRU_API int sru_scan_backward(const float* U, const float* X, const float* C, co
  * ------------------------------------------------------------------------- */
 typedef enum { SRU_DTYPE_FP32 = 0, SRU_DTYPE_BF16 = 1 } sru_dtype;
 
-/* Vocabulary rows: logits [N, V], row pitch ld >= V elements, columns
+/* Vocabulary rows: logits [N, V] (V < 2^30), row pitch ld >= V elements, columns
  * contiguous, at a temperature T > 0 (finite, and so is log2(e) / T):
  *   m = max_j z_j,  S = sum_j exp((z_j - m) / T),
  *   log p_j = (z_j - m) / T - log S
@@ -470,7 +470,9 @@ SRU_API int sru_residual_norm_backward(int M, int d, int dtype, int res_dtype, i
  * few channels are cut into chunks whose maps go through the workspace; results
  * are the same in every run.
  * A sequence cut into consecutive calls (h_last -> h0) agrees with one call to
- * fp32 rounding. */
+ * fp32 rounding.
+ * Sizes: L * B below 2^31 - 1024, B * d below 2^31, and the workgroups below 2^22:
+ * B ceil(d / 64), up to 256 times as many where a sequence is cut. */
 #define SRU_LRU_STEPS 8
 SRU_API size_t sru_lru_forward_workspace_bytes(int L, int B, int d);
 SRU_API int sru_lru_forward(int L, int B, int d, int dtype, const void* x, long long x_t,

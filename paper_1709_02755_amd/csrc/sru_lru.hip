@@ -25,11 +25,14 @@
 // What bounds it: memory, with the gates' arithmetic close behind (39 vector
 // instructions an element forward, 5 of them exp, rcp or sqrt; the vector units are
 // busy 46 % of the time forward, 50 % of the gradient's).  L 256, B 64, d 1024 in
-// bf16: 32 us for 134 MB (4.2 TB/s) and 61 us for 235 MB (3.9), where a large copy
-// makes 5.4.  L 32768, B 1, d 1024: 110 us and 143 us, for three quarters more to
-// read forward and a third more in the gradient than in one pass; workgroups that
-// handed on their state to the next one through memory read everything once, but
-// took 114 and 171 us: a state needs 2 to 3 us from one workgroup to the next.
+// bf16, each call repeated by itself: 32 us for 134 MB (4.2 TB/s) and 61 us for 235
+// MB (3.9), where a copy that moves as much makes 6.4; in a training step, forward
+// and gradient in turn, the kernels take 36 and 52 + 5, the gradient's with part of
+// its inputs still in the caches.  L 32768, B 1, d 1024: 110 us and 144 us (in turn 61
+// + 63 and 35 + 111 + 5), for three quarters more to read forward and a third more
+// in the gradient than in one pass; workgroups that handed on their state to the
+// next one through memory read everything once, but took 114 and 171 us: a state
+// needs 2 to 3 us from one workgroup to the next.
 //
 // A map with A = 0 forgets what came before: that is how a new document's
 // start, and a state that is known, are written (a state of NaN before a new
@@ -797,7 +800,7 @@ __global__ __launch_bounds__(1024) void lru_sums_kernel(LruArgs a, const float* 
 }
 
 // How a call is cut, by its groups of 64 channels of a sequence (us, bf16, forward
-// and gradient, one box):
+// and gradient, each call repeated by itself on one box):
 // - many: two channels a lane, small workgroups, which overlap each other's loads
 //   and arithmetic.  L 256, B 64, d 1024 (1,024 groups): 32 / 61; workgroups of 16
 //   and 8 waves of one channel a lane 44 / 70.

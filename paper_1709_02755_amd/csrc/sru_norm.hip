@@ -7,8 +7,10 @@
 // in 16-byte loads (but see by_width), its sums are taken there, and the
 // results leave rounded once.  The gradient works x' out again from x, y and z
 // rather than reading x_out, so that no rounded value enters it.  16384 x 1024,
-// bf16 beside an fp32 residual: 50 us for 235 MB (4.7 TB/s) and 88 us for 369 MB (4.2
-// TB/s); 8 x 1024 bf16: 4.4 us, a launch.
+// bf16 beside an fp32 residual, each call repeated by itself: 50 us for 235 MB (4.7
+// TB/s) and 88 us for 369 MB (4.2 TB/s); in turn, as in training, the kernels take 49
+// and 76 + 5, the gradient's with part of its inputs still in the caches.  8 x 1024
+// bf16: 4.4 us, a launch.
 #include <type_traits>
 
 #include "sru_device.h"

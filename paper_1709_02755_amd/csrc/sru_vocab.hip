@@ -461,11 +461,13 @@ __device__ __forceinline__ void top_write(const LogprobArgs& a, int row, const R
 // floats, then [row, part, K] pairs.
 //
 // Without alternatives it reads at 4.9 TB/s (2048 x 65536 bf16, 54 us) and is
-// bound by that.  With five, 1000 x 30011 fp32 takes 35 us (3.5 TB/s): the first
-// vectors of a row fill the lists before there is a bound, and all rows are at it
-// at the same time.  Twenty of 4 x 131072 bf16, in eight parts a row, take 11.5 us and
-// 6.4 to join: launches and waits, one after the other.  Loads a round ahead were
-// slower in every case (1000 x 30011 26 -> 27 us, with alternatives 39 -> 52).
+// bound by that.  With alternatives, 1000 x 30011 fp32 takes 31, 34, 39 and 45 us for
+// 1, 5, 20 and 64 of them, and 27 without: what passes the bounds is collected, cut
+// and ranked by all rows at about the same time.  The bounds after the first round
+// cost less than 1 us of that and save more (without them 31, 37, 48 and 130).
+// Twenty of 4 x 131072 bf16, in eight parts a row, take 11.4 us and 6.7 to join:
+// launches and waits, one after the other.  Loads a round ahead were slower in every
+// case (1000 x 30011 26 -> 27 us, with alternatives 39 -> 52).
 // Six waves on a SIMD rather than the five that the compiler would leave: three
 // workgroups fit a CU (4096 x 32768 bf16, five alternatives, 90 -> 80 us).
 template <bool BF16, int THREADS, int U, bool TOP>
@@ -693,7 +695,7 @@ struct PointTerms {
 
 // dz_j = (1/T) (w_t [j = t] + sum_k w_k [j = id_k] - p_j A - dH p_j (log p_j + H)),
 // A = w_t + sum_k w_k, with p = e / S and log p = x ln2 - log S.
-// Bound by memory: 2048 x 65536 bf16 in 81 us, 268 MB read (partly from the caches,
+// Bound by memory: 2048 x 65536 bf16 in 85 us, 268 MB read (partly from the caches,
 // after the forward) and as many written.
 template <bool BF16, int THREADS, int U>
 __global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LogprobGradArgs a, int parts) {
@@ -846,8 +848,10 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, const float*
 // (4.7 TB/s read and written), both at once 270: a row's second read comes from
 // the caches, which the rows that run at a time (three to a CU) fit.  Holding a row in
 // registers between its two uses was slower: only one then fits a CU, and its
-// loads stop while it writes.  515 x 30011 fp32: 16 and 25 us; all rows run at
-// the same time there, and none reads while they join their sums and the teacher's.
+// loads stop while it writes.  515 x 30011 fp32: 16 and 25 us, 700 x 30011 17 and 38,
+// both at once 44; these rows are too many to be cut and few enough to run all at the
+// same time, two or three to a CU, so that none reads while they join their sums and
+// the teacher's.
 template <bool BF16, int THREADS, int U, bool STATS, bool GRAD>
 __global__ __launch_bounds__(THREADS, 6) void distill_kernel(DistillArgs a, int parts) {
   using E = Elem<BF16>;
@@ -944,7 +948,7 @@ constexpr int kThreads = 512;
 constexpr int kFewThreads = 256;
 constexpr int kUnroll = 4;
 
-// Parts a row is cut into where there are fewer rows than CUs.  Those of a
+// Parts a row is cut into where there are fewer rows than two to a CU.  Those of a
 // gradient have at least a round of vectors; those of statistics, which another
 // launch has to join, one for every load in flight, and a row of fewer than four
 // such parts is left whole: the launch costs more than the rounds (us, cut and

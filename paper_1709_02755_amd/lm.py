@@ -452,7 +452,8 @@ def lru_forward(x, r, i, lam, h0=None, mask=None, reset=None, c=8.0, keep_states
     nonzero where a new document starts (a = 0).  Returns dict(H [L, B, d],
     h_last [B, d], states): states, the state before every LRU_STEPS-th step,
     is what lru_backward needs (None with keep_states=False).  x, r, i and H
-    may be strided: slices of one projection, or [B, L, d] transposed."""
+    may be strided: slices of one projection, or [B, L, d] transposed.  out may
+    hold H, h_last (h0 itself: the state taken on in place) and states."""
     shape, code, dv, (sx, sr, si) = _lru_inputs(x, r, i, lam, mask, reset)
     L, B, d = shape
     _req(h0, "h0", (B, d), optional=True, device=dv)
