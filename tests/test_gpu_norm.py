@@ -370,6 +370,21 @@ def test_rows_past_32_bits():
     assert torch.equal(f2["o"], fw["o"]) and torch.equal(y, g["dy"])
 
 
+@pytest.mark.parametrize("d", [1032, 1033])
+def test_more_rows_than_a_launch_has_workgroups(d):
+    """Rows that a workgroup comes to after its first: the bits of the same rows in
+    a call of their own."""
+    M, last = (1 << 20) + 9, 20
+    y = torch.randn((M, d), device="cuda").to(B16)
+    w = torch.linspace(0.5, 1.5, d, device="cuda")
+    p = dict(w_post=w, scale=w, w_pre=w, eps=EPS)
+    whole = lm.residual_norm_forward(y, y, z=y, **p)
+    end = y[M - last:].clone()
+    part = lm.residual_norm_forward(end, end, z=end, **p)
+    for n in ("x_out", "o", "rstd"):
+        assert torch.equal(whole[n][M - last:], part[n]), n
+
+
 def test_refusals():
     t = dev(inputs(4, 32, B16, F32, 1))
     p = dict(w_pre=t["w_pre"])

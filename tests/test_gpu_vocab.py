@@ -140,6 +140,23 @@ def test_logprobs_and_gradient(N, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V", [(2, 64), (3, 5003), (2, 70001)])
+def test_most_alternatives_and_their_gradient(N, V, dtype):
+    T, top = 1.2, lm.MAX_TOP
+    g = torch.Generator().manual_seed(V)
+    tokens = torch.randint(0, V, (N,), generator=g).cuda()
+    z = rows(N, V, dtype, V + 1)
+    fw = check_logprobs(z, tokens, top, T)
+    _, ent, ids, _, lp, p = plain(z, tokens, top, T)
+    tokens[0] = ids[0, 5]  # one of the alternatives
+    dlp, dtop = torch.randn(N, generator=g), torch.randn((N, top), generator=g)
+    got = lm.token_logprobs_backward(z, tokens, fw, dlp.cuda(), None, dtop.cuda(), temperature=T)
+    ref = grad_plain(z, tokens, ids, lp, p, ent, dlp, None, dtop, T)
+    weight = dlp.double().abs() + dtop.double().abs().sum(1)
+    close("dlogits", got, ref, (weight / T)[:, None], dtype == torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("pitch,offset", [(1003, 1), (1003, 5), (1008, 3), (1001, 0)])
 def test_strided_rows(pitch, offset, dtype):
     """Rows whose starts differ in alignment, read and written in place and
@@ -373,6 +390,38 @@ def test_rows_past_32_bits():
     ref = lm.token_logprobs_backward(z.contiguous(), tokens, fw, dlp)
     lm.token_logprobs_backward(z, tokens, fw, dlp, dlogits=z)
     assert torch.equal(z, ref)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [9, 64])
+def test_more_rows_than_a_launch_has_workgroups(V, dtype):
+    """Rows that a workgroup comes to after its first: the bits of the same rows in
+    a call of their own."""
+    N, K, T, last = (1 << 20) + 37, 3, 0.8, 50
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.randn((N, V), generator=g, device="cuda").to(dtype)
+    tokens = torch.randint(-1, V, (N,), generator=g, device="cuda")
+    ids = torch.randint(-1, V, (N, K), generator=g, device="cuda")
+    t = torch.randn((N, K), generator=g, device="cuda")
+    dl = torch.randn(N, generator=g, device="cuda")
+    dtop = torch.randn((N, K), generator=g, device="cuda")
+
+    def step(z, tokens, ids, t, dl, dtop):
+        fw = lm.token_logprobs(z, tokens, top=K, temperature=T)
+        plain_fw = lm.token_logprobs(z, tokens, temperature=T)
+        b = lm.distill_forward_backward(z, ids, t, dl, temperature=T)
+        two = lm.distill_forward(z, ids, t, temperature=T)
+        return [fw["logprob"], fw["entropy"], fw["top_ids"], fw["top_logprobs"],
+                plain_fw["logprob"],
+                lm.token_logprobs_backward(z, tokens, fw, dl, dl, dtop, temperature=T),
+                b["loss"], b["dlogits"], two["loss"],
+                lm.distill_backward(z, ids, t, two["stats"], dl, temperature=T)]
+
+    args = z, tokens, ids, t, dl, dtop
+    whole = step(*args)
+    part = step(*(a[N - last:].contiguous() for a in args))
+    for a, b in zip(whole, part):
+        assert torch.equal(a[N - last:], b)
 
 
 def test_refusals():
